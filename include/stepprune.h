@@ -14,11 +14,15 @@
  *   stepprune_compact  step 5: physical gather of the kept tokens ahead of the
  *                      prompt into a padded or packed prefill buffer.
  * Beside them: stepprune_encode, the cross-modal input encoder of Eq. 3 that
- * turns X into the candidate tokens H ahead of step 1; and, for the training
+ * turns X into the candidate tokens H ahead of step 1; for the training
  * pathway (Section "Trajectory-Aware Differentiable Optimization"),
  * stepprune_select_trajectory (the trajectory sums of Eqs. 5-7) and
  * stepprune_gate_denoise (the noise gate of Eq. 9 and the locally masked
- * denoiser).
+ * denoiser); and, for the language model that reads the compacted buffer,
+ * stepprune_compact_positions (the positions of its rows),
+ * stepprune_cache_append (keys and values into a paged cache, rotated by
+ * position) and stepprune_cache_attend (attention over the cache, a prefix that
+ * several sequences share computed once for all of them).
  *
  * Conventions shared by every call
  *  - Pointers are DEVICE pointers unless marked (host).  All row-major.
@@ -105,7 +109,9 @@ enum {
   SP_DEV_BAD_OFFSETS = 1,   /* an offset array is not non-decreasing or exceeds its total */
   SP_DEV_GROUP_TOO_LARGE = 2,/* a group has more tokens than max_group */
   SP_DEV_BAD_CAP = 3,       /* a group cap is negative or exceeds max_cap */
-  SP_DEV_OUTPUT_OVERFLOW = 4 /* kept or prefill rows exceed the capacity given */
+  SP_DEV_OUTPUT_OVERFLOW = 4,/* kept or prefill rows exceed the capacity given */
+  SP_DEV_BAD_PAGE = 5,      /* a page of a run lies outside the cache */
+  SP_DEV_BAD_POSITION = 6   /* a position lies outside the table of angles */
 };
 
 /* Shapes shared by the calls (host). d, d_text and h are multiples of 64,
@@ -440,6 +446,154 @@ sp_status stepprune_encode(const sp_dims* dims, const void* X, int64_t T_vis,
                            const sp_encoder_block* blocks, int32_t max_seq, uint32_t flags,
                            void* H, void* ws, size_t ws_bytes,
                            const hipEvent_t* events, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * The cache: what the language model does with the compacted buffer.
+ *
+ * Keys and values live in two arrays of pages, each [pages, kv_heads,
+ * page_size, head_dim], page_size tokens of one run to a page.  A run is a
+ * sequence of tokens in pages of its own; slot p of run s is place
+ * p % page_size of page table[s][p / page_size].  A batch's sequences are runs;
+ * so are the prefixes that groups of them share (several questions about one
+ * image: its compacted rows are the prefix, its pages are read once for all).
+ *
+ * Rows of the model's q, k and v products are described as the compaction
+ * leaves them: packed (seq_info = cu_seqlens [S+1]) or padded (seq_info [S] =
+ * row counts, sequence s at row s rows_per_seq).  Rows that belong to no
+ * sequence are neither read nor written.  One token per sequence is the same
+ * with one row each.
+ *
+ * dtype (SP_BF16, SP_F32) applies to q, k, v, the cache and the output; scores,
+ * softmax, sums and angles are float32.
+ */
+typedef struct {
+  int32_t q_heads;     /* <= 1024, a multiple of kv_heads: query head j reads key head j / (q_heads / kv_heads) */
+  int32_t kv_heads;
+  int32_t head_dim;    /* 64 or 128 (SP_EUNSUPPORTED otherwise) */
+  int32_t dtype;       /* sp_dtype */
+  int32_t page_size;   /* 16, 32, 64, 128 or 256 (SP_EUNSUPPORTED otherwise) */
+  int32_t pages;       /* pages of the cache, >= 1 */
+} sp_cache_dims;
+
+/* The rows of a batch (host struct). */
+typedef struct {
+  int64_t rows;             /* rows of the arrays; rows (q_heads / kv_heads) < 2^26 */
+  int32_t layout;           /* SP_LAYOUT_PACKED or SP_LAYOUT_PADDED */
+  int32_t rows_per_seq;     /* padded: rows of a sequence's slice; packed: ignored */
+  const int32_t* seq_info;  /* device: packed [S+1] offsets from 0, padded [S] counts */
+  int32_t max_rows;         /* upper bound on any sequence's rows */
+} sp_cache_rows;
+
+/* Runs of the cache (host struct). */
+typedef struct {
+  const int32_t* table;     /* device [count, table_width]: the pages of each run; entries past a
+                               run's tokens are not used */
+  const int32_t* len;       /* device [count]: tokens of each run, new rows included, so the first
+                               new row of sequence s has slot len[s] - (its rows) */
+  int32_t count;            /* S for the sequences, G for the prefixes */
+  int32_t table_width;
+  int32_t max_len;          /* upper bound on any len, <= table_width page_size; a longer run is a
+                               device error (SP_DEV_GROUP_TOO_LARGE) and its outputs are undefined */
+} sp_cache_runs;
+
+/* Rotation of q and k by position (host struct).  Pair j of a head's first
+ * rot_dim elements, (x_j, x_{j + rot_dim/2}) or, interleaved, (x_{2j},
+ * x_{2j+1}), becomes (x c - x' s, x' c + x s) with (c, s) = cos_sin[p][j], p
+ * the row's position on the pair's axis: pairs [0, section[0]) follow axis 0,
+ * the next section[1] axis 1, the next section[2] axis 2. */
+typedef struct {
+  const float* cos_sin;     /* device [positions, rot_dim / 2, 2], 16-byte aligned */
+  int32_t positions;        /* a position outside [0, positions) is a device error
+                               (SP_DEV_BAD_POSITION); its row is left out */
+  int32_t rot_dim;          /* a multiple of 16, <= head_dim */
+  int32_t interleaved;      /* 0 or 1 */
+  const int32_t* pos;       /* device [axes, rows], or NULL: the row's slot */
+  int32_t axes;             /* 1 to 3 (pos NULL: 1) */
+  int32_t section[3];       /* pairs of each axis, rot_dim / 2 in all */
+} sp_cache_rotation;
+
+/*
+ * Positions of the compacted buffer's rows: what stepprune_compact does to rows,
+ * done to their positions, on 1 to 3 axes:
+ *   pos[a][row of kept token i of image b] = vis_pos[a][img_off[b] + i],
+ *   pos[a][row of text row t]              = text_pos[a][t].
+ *  vis_pos [axes, T_vis], text_pos [axes, T_txt]  positions before pruning
+ *  pos     out [axes, out_rows] int32; rows that stepprune_compact leaves
+ *          untouched are left untouched
+ *  Offsets, kept tokens, layout and ws as for stepprune_compact; inconsistent
+ *  ones are recorded alike.
+ */
+sp_status stepprune_compact_positions(const int32_t* vis_pos, int64_t T_vis, const int32_t* img_off,
+                                      const int32_t* text_pos, int64_t T_txt, const int32_t* text_off,
+                                      int32_t axes, const int32_t* kept_idx, const int32_t* kept_off,
+                                      const int32_t* kept_cnt, int32_t B, int32_t layout,
+                                      int32_t rows_per_image, int64_t out_rows, int32_t* pos,
+                                      void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Appends the batch's keys and values to their runs, the keys rotated by
+ * position, and rotates the queries: row i of sequence s goes to slot
+ * len[s] - n_s + i.
+ *
+ *  Q [rows, q_heads head_dim], K and V [rows, kv_heads head_dim] with row
+ *          strides ldq, ldk, ldv in elements (a fused product's columns, for
+ *          example); pointers and strides 16-byte aligned
+ *  rot     NULL: nothing is rotated
+ *  Q_out   out [rows, q_heads head_dim], contiguous; may be Q when ldq is
+ *          q_heads head_dim.  Q and Q_out NULL: only keys and values
+ *  k_cache, v_cache  out, the slots of the batch's rows only
+ *  ws      256 bytes, for the error word
+ * Every element is rounded once.  Two rows with one slot are a race of the
+ * caller's.
+ */
+sp_status stepprune_cache_append(const sp_cache_dims* dims, const void* Q, int64_t ldq,
+                                 const void* K, int64_t ldk, const void* V, int64_t ldv,
+                                 const sp_cache_rows* rows, const sp_cache_runs* runs,
+                                 const sp_cache_rotation* rot, void* Q_out, void* k_cache,
+                                 void* v_cache, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Flags of stepprune_cache_attend. */
+enum { SP_ATTEND_ALL = 1u };  /* every row sees its sequence's whole run */
+
+/*
+ * Attention of the batch's query rows over the cache.  Row i of sequence s (n_s
+ * rows, a run of L_s tokens) sees its group's prefix run, whole, and the
+ * tokens j of its own run with j < L_s - n_s + i + 1 (with SP_ATTEND_ALL
+ * j < L_s):
+ *   o = sum_j softmax_j(scale <q, k_j>) v_j,   lse = log sum_j exp(scale <q, k_j>).
+ * A row that sees no token (or only scores of -inf) gives o = 0, lse = -inf.
+ * Tokens that a row does not see have no influence on it, whatever their pages
+ * hold.  A prefix is read once for the rows of all its sequences.  With
+ * prefixes and runs of length 0 this is cross attention to the prefixes.
+ *
+ *  Q        [rows, q_heads head_dim], row stride ldq; 16-byte aligned
+ *  rows, runs   the batch's sequences (runs->count = S)
+ *  prefix   the prefix runs (count = G), or NULL: none
+ *  grp_off  [G+1] device, ascending: group g is sequences [grp_off[g],
+ *           grp_off[g+1]); sequences outside every group have no prefix.
+ *           NULL with prefix NULL
+ *  scale    > 0; neither it nor scale log2(e) infinite or denormal
+ *  O        out [rows, q_heads head_dim], contiguous; may not alias Q
+ *  lse      out [rows, q_heads] float32, or NULL
+ *  ws       stepprune_cache_workspace_bytes() bytes, the error word first; one
+ *           call at a time may use it
+ *  events   [0] before, [1] after the whole call (or NULL)
+ * The bounds rows, max_rows and max_len (not the lengths) decide the split of
+ * the work, so a captured call stays right while the lengths grow up to them;
+ * lengths far below their bounds cost launches that find nothing to do.
+ * Probabilities weight the values rounded to dtype; all sums are float32.
+ */
+sp_status stepprune_cache_attend(const sp_cache_dims* dims, const void* Q, int64_t ldq,
+                                 const sp_cache_rows* rows, const sp_cache_runs* runs,
+                                 const sp_cache_runs* prefix, const int32_t* grp_off, float scale,
+                                 uint32_t flags, const void* k_cache, const void* v_cache, void* O,
+                                 float* lse, void* ws, size_t ws_bytes, const hipEvent_t* events,
+                                 hipStream_t stream);
+
+/* Workspace bytes of stepprune_cache_attend for these bounds (device pointers in
+   the structs are not read).  Returns 0 for invalid arguments. */
+size_t stepprune_cache_workspace_bytes(const sp_cache_dims* dims, const sp_cache_rows* rows,
+                                       const sp_cache_runs* runs, const sp_cache_runs* prefix);
 
 /* Workspace bytes for stage `which` (0 project, 1 select, 2 compact, 3 gate
    and denoiser, 4 input encoder; for 3, T_vis is the token count T; for 4,

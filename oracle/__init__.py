@@ -17,6 +17,7 @@ Modules
   compaction   Algorithm 1 step 5: gather of kept tokens ahead of the prompt
   denoise      the training pathway's noise gate (Eq. 9) and masked denoiser
   encoder      the cross-modal input encoder (Eq. 3)
+  cache        positions of compacted rows, the paged cache's append and attention
   calibration  the STOP bias that gives a target mean retained count
 
 Every function states the passage it follows.  Readings of points the paper

@@ -18,11 +18,15 @@ SP_F32, SP_BF16 = 0, 1
 SP_TRACE, SP_NO_HISTORY, SP_FULL_ROLLOUT, SP_GRAM_ONLY, SP_REUSE_GRAM, SP_LOGITS = 1, 2, 4, 8, 16, 32
 SP_LAYOUT_PADDED, SP_LAYOUT_PACKED = 0, 1
 SP_DEV_OK, SP_DEV_BAD_OFFSETS, SP_DEV_GROUP_TOO_LARGE, SP_DEV_BAD_CAP, SP_DEV_OUTPUT_OVERFLOW = range(5)
+SP_DEV_BAD_PAGE, SP_DEV_BAD_POSITION = 5, 6
+SP_ATTEND_ALL = 1
 STAGE_PROJECT, STAGE_SELECT, STAGE_COMPACT = 0, 1, 2
 
 EXPORTS = ["stepprune_project", "stepprune_select", "stepprune_select_trajectory", "stepprune_compact",
            "stepprune_gate_denoise", "stepprune_workspace_bytes", "stepprune_read_device_error",
-           "stepprune_status_string", "stepprune_select_noalloc", "stepprune_encode"]
+           "stepprune_status_string", "stepprune_select_noalloc", "stepprune_encode",
+           "stepprune_compact_positions", "stepprune_cache_append", "stepprune_cache_attend",
+           "stepprune_cache_workspace_bytes"]
 STAGE_ENCODE = 4
 SP_ENC_CAUSAL = 1
 ENCODER_FIELDS = ("ln1_g", "ln1_b", "W_qkv", "b_qkv", "W_o", "b_o", "ln2_g", "ln2_b", "W_1", "b_1",
@@ -56,6 +60,27 @@ class sp_denoiser(ctypes.Structure):
 
 class sp_encoder_block(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ENCODER_FIELDS]
+
+
+class sp_cache_dims(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("q_heads", "kv_heads", "head_dim", "dtype", "page_size",
+                                              "pages")]
+
+
+class sp_cache_rows(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("layout", ctypes.c_int32), ("rows_per_seq", ctypes.c_int32),
+                ("seq_info", ctypes.c_void_p), ("max_rows", ctypes.c_int32)]
+
+
+class sp_cache_runs(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("len", ctypes.c_void_p), ("count", ctypes.c_int32),
+                ("table_width", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+
+
+class sp_cache_rotation(ctypes.Structure):
+    _fields_ = [("cos_sin", ctypes.c_void_p), ("positions", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("pos", ctypes.c_void_p), ("axes", ctypes.c_int32),
+                ("section", ctypes.c_int32 * 3)]
 
 
 if not os.path.exists(LIB_PATH):
@@ -95,6 +120,19 @@ _lib.stepprune_encode.argtypes = [_DIMS, _P, _I64, _P, _I32, _P, _P, _I64, _P, _
                                   _SZ, _P, _P]
 _lib.stepprune_workspace_bytes.restype = _SZ
 _lib.stepprune_workspace_bytes.argtypes = [_I32, _DIMS, _I64, _I64, _I32, _I32, _I32, _I32]
+_CACHE, _ROWS, _RUNS, _ROT = (ctypes.POINTER(t) for t in (sp_cache_dims, sp_cache_rows, sp_cache_runs,
+                                                           sp_cache_rotation))
+_lib.stepprune_compact_positions.restype = _I32
+_lib.stepprune_compact_positions.argtypes = [_P, _I64, _P, _P, _I64, _P, _I32, _P, _P, _P, _I32, _I32, _I32,
+                                             _I64, _P, _P, _SZ, _P]
+_lib.stepprune_cache_append.restype = _I32
+_lib.stepprune_cache_append.argtypes = [_CACHE, _P, _I64, _P, _I64, _P, _I64, _ROWS, _RUNS, _ROT, _P, _P, _P,
+                                        _P, _SZ, _P]
+_lib.stepprune_cache_attend.restype = _I32
+_lib.stepprune_cache_attend.argtypes = [_CACHE, _P, _I64, _ROWS, _RUNS, _RUNS, _P, _F32, ctypes.c_uint32, _P,
+                                        _P, _P, _P, _P, _SZ, _P, _P]
+_lib.stepprune_cache_workspace_bytes.restype = _SZ
+_lib.stepprune_cache_workspace_bytes.argtypes = [_CACHE, _ROWS, _RUNS, _RUNS]
 _lib.stepprune_read_device_error.restype = _I32
 _lib.stepprune_read_device_error.argtypes = [_P, _P, ctypes.POINTER(_I32)]
 _lib.stepprune_status_string.restype = ctypes.c_char_p
@@ -238,6 +276,62 @@ def stepprune_encode(dm, X, T_vis, img_off, B, E_text, text_off, T_txt, W_p, g_t
                                _ptr(text_off), T_txt, _ptr(W_p), g_text, blocks, max_seq, flags,
                                _ptr(H), _ptr(ws), ws_bytes, _events(events), _stream(stream))
     return _check("stepprune_encode", st, raise_on_error)
+
+
+def cache_dims(q_heads, kv_heads, head_dim, dtype, page_size, pages) -> sp_cache_dims:
+    return sp_cache_dims(q_heads, kv_heads, head_dim, dtype, page_size, pages)
+
+
+def cache_rows(rows, layout, rows_per_seq, seq_info, max_rows) -> sp_cache_rows:
+    """The rows of a batch (``seq_info`` device int32, as the compaction writes it)."""
+    return sp_cache_rows(rows, layout, rows_per_seq, _ptr(seq_info), max_rows)
+
+
+def cache_runs(table, length, max_len) -> sp_cache_runs:
+    """Runs of the cache: device int32 ``table`` [count, width] and ``length`` [count]."""
+    return sp_cache_runs(_ptr(table), _ptr(length), table.shape[0], table.shape[1], max_len)
+
+
+def cache_rotation(cos_sin, rot_dim, pos=None, section=None, interleaved=False) -> sp_cache_rotation:
+    """Rotation by position: float32 ``cos_sin`` [positions, rot_dim / 2, 2]; int32 ``pos``
+    [axes, rows] with the pairs of each axis in ``section``, or None: the rows' slots."""
+    section = [rot_dim // 2] if section is None else list(section)
+    return sp_cache_rotation(_ptr(cos_sin), cos_sin.shape[0], rot_dim, 1 if interleaved else 0, _ptr(pos),
+                             len(section), (_I32 * 3)(*(section + [0] * (3 - len(section)))))
+
+
+def _ref(struct):
+    return None if struct is None else ctypes.byref(struct)
+
+
+def stepprune_compact_positions(vis_pos, T_vis, img_off, text_pos, T_txt, text_off, axes, kept_idx,
+                                kept_off, kept_cnt, B, layout, rows_per_image, out_rows, pos, ws,
+                                ws_bytes, stream=None, raise_on_error=True):
+    st = _lib.stepprune_compact_positions(_ptr(vis_pos), T_vis, _ptr(img_off), _ptr(text_pos), T_txt,
+                                          _ptr(text_off), axes, _ptr(kept_idx), _ptr(kept_off),
+                                          _ptr(kept_cnt), B, layout, rows_per_image, out_rows, _ptr(pos),
+                                          _ptr(ws), ws_bytes, _stream(stream))
+    return _check("stepprune_compact_positions", st, raise_on_error)
+
+
+def stepprune_cache_append(dm, Q, ldq, K, ldk, V, ldv, rows, runs, rot, Q_out, k_cache, v_cache, ws,
+                           ws_bytes, stream=None, raise_on_error=True):
+    st = _lib.stepprune_cache_append(_ref(dm), _ptr(Q), ldq, _ptr(K), ldk, _ptr(V), ldv, _ref(rows),
+                                     _ref(runs), _ref(rot), _ptr(Q_out), _ptr(k_cache), _ptr(v_cache),
+                                     _ptr(ws), ws_bytes, _stream(stream))
+    return _check("stepprune_cache_append", st, raise_on_error)
+
+
+def stepprune_cache_workspace_bytes(dm, rows, runs, prefix=None) -> int:
+    return int(_lib.stepprune_cache_workspace_bytes(_ref(dm), _ref(rows), _ref(runs), _ref(prefix)))
+
+
+def stepprune_cache_attend(dm, Q, ldq, rows, runs, prefix, grp_off, scale, flags, k_cache, v_cache, O,
+                           lse, ws, ws_bytes, stream=None, raise_on_error=True, events=None):
+    st = _lib.stepprune_cache_attend(_ref(dm), _ptr(Q), ldq, _ref(rows), _ref(runs), _ref(prefix),
+                                     _ptr(grp_off), scale, flags, _ptr(k_cache), _ptr(v_cache), _ptr(O),
+                                     _ptr(lse), _ptr(ws), ws_bytes, _events(events), _stream(stream))
+    return _check("stepprune_cache_attend", st, raise_on_error)
 
 
 def stepprune_read_device_error(ws, stream=None) -> int:

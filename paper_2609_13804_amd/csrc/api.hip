@@ -1,6 +1,7 @@
 // C ABI of libstepprune (include/stepprune.h): host-side validation, workspace
 // layout and launch order.  Every entry point validates its arguments before
 // touching the device and never throws.
+#include <float.h>
 #include <string.h>
 
 #include <mutex>
@@ -106,6 +107,84 @@ sp_status check_encode_dims(const sp_dims* d) {
   if (st != SP_OK) return st;
   if (d->dtype != SP_BF16 || d->d % 128 || d->d > 4096) return SP_EUNSUPPORTED;
   return SP_OK;
+}
+
+// The cache's structs, checked into the kernels' form.
+sp_status check_cache_dims(const sp_cache_dims* d, CacheShape& s) {
+  if (!d) return SP_EINVAL;
+  if (d->q_heads < 1 || d->kv_heads < 1 || d->q_heads % d->kv_heads || d->head_dim < 1 ||
+      d->page_size < 1 || d->pages < 1)
+    return SP_EINVAL;
+  if (d->dtype != SP_F32 && d->dtype != SP_BF16) return SP_EUNSUPPORTED;
+  if (d->head_dim != 64 && d->head_dim != 128) return SP_EUNSUPPORTED;
+  if (d->q_heads > kMaxCacheHeads) return SP_EUNSUPPORTED;
+  s.page_shift = 4;
+  while (s.page_shift < 8 && (1 << s.page_shift) != d->page_size) ++s.page_shift;
+  if ((1 << s.page_shift) != d->page_size) return SP_EUNSUPPORTED;
+  s.q_heads = d->q_heads;
+  s.kv_heads = d->kv_heads;
+  s.head_dim = d->head_dim;
+  s.dtype = d->dtype;
+  s.pages = d->pages;
+  return SP_OK;
+}
+
+// Device pointers are looked at only with `pointers` (the workspace query has none).
+sp_status check_cache_runs(const sp_cache_runs* r, const CacheShape& s, bool pointers, CacheRuns& o) {
+  if (!r) return SP_EINVAL;
+  if (r->count < 0 || r->table_width < 0 || r->max_len < 0) return SP_EINVAL;
+  if (r->max_len > (int64_t)r->table_width << s.page_shift) return SP_EINVAL;
+  if (pointers && r->count > 0 && (!r->len || (r->max_len > 0 && !r->table))) return SP_EINVAL;
+  o.table = r->table;
+  o.len = r->len;
+  o.count = r->count;
+  o.width = r->table_width;
+  o.max_len = r->max_len;
+  return SP_OK;
+}
+
+sp_status check_cache_rows(const sp_cache_rows* r, const CacheShape& s, int S, bool pointers, CacheRows& o) {
+  if (!r) return SP_EINVAL;
+  if (r->rows < 0 || r->max_rows < 0) return SP_EINVAL;
+  if (r->layout != SP_LAYOUT_PADDED && r->layout != SP_LAYOUT_PACKED) return SP_EINVAL;
+  o.padded = r->layout == SP_LAYOUT_PADDED;
+  if (o.padded && (r->rows_per_seq < 0 || (int64_t)r->rows_per_seq * S > r->rows)) return SP_EINVAL;
+  if (pointers && S > 0 && !r->seq_info) return SP_EINVAL;
+  if (r->rows > (int64_t)kMaxCacheRows / (s.q_heads / s.kv_heads)) return SP_EUNSUPPORTED;
+  o.rows = r->rows;
+  o.rows_per_seq = o.padded ? r->rows_per_seq : 0;
+  o.info = r->seq_info;
+  // no sequence is longer than its slice or the arrays, however large a bound is passed
+  const int64_t most = o.padded ? o.rows_per_seq : o.rows;
+  o.max_rows = r->max_rows < most ? r->max_rows : (int)most;
+  return SP_OK;
+}
+
+sp_status check_attend(const sp_cache_dims* dims, const sp_cache_rows* rows, const sp_cache_runs* runs,
+                       const sp_cache_runs* prefix, bool pointers, AttendArgs& a) {
+  sp_status st = check_cache_dims(dims, a.shape);
+  if (st == SP_OK) st = check_cache_runs(runs, a.shape, pointers, a.runs);
+  if (st == SP_OK) st = check_cache_rows(rows, a.shape, a.runs.count, pointers, a.rows);
+  a.prefix = CacheRuns{};
+  if (st == SP_OK && prefix) st = check_cache_runs(prefix, a.shape, pointers, a.prefix);
+  if (st == SP_OK) a.plan = plan_cache_attend(a.shape, a.rows, a.runs, a.prefix);
+  return st;
+}
+
+// Header; parts of every row; the parts' maxima and sums, and their outputs,
+// [rows][q_heads][parts] (none where a row has one part at most, which is its output).
+struct AttendWs {
+  size_t row_parts, ml, o, total;
+};
+AttendWs attend_ws_layout(const AttendArgs& a) {
+  AttendWs w;
+  const size_t parts = (size_t)a.plan.prefix_parts + a.plan.own_parts;
+  const size_t n = parts > 1 || a.plan.prefix_parts ? (size_t)a.rows.rows * a.shape.q_heads * parts : 0;
+  w.row_parts = kWsHeaderBytes;
+  w.ml = align_up(w.row_parts + (size_t)a.rows.rows * 4, 256);
+  w.o = align_up(w.ml + n * 2 * 4, 256);
+  w.total = align_up(w.o + n * a.shape.head_dim * 4, 256);
+  return w;
 }
 
 }  // namespace
@@ -391,6 +470,150 @@ sp_status stepprune_compact(const sp_dims* dims, const void* X, const int32_t* i
   a.err = reinterpret_cast<int32_t*>(ws);
   record_event(events, 0, stream);
   hipError_t e = launch_compact(a, stream);
+  record_event(events, 1, stream);
+  return hip_status(e);
+}
+
+sp_status stepprune_compact_positions(const int32_t* vis_pos, int64_t T_vis, const int32_t* img_off,
+                                      const int32_t* text_pos, int64_t T_txt, const int32_t* text_off,
+                                      int32_t axes, const int32_t* kept_idx, const int32_t* kept_off,
+                                      const int32_t* kept_cnt, int32_t B, int32_t layout,
+                                      int32_t rows_per_image, int64_t out_rows, int32_t* pos,
+                                      void* ws, size_t ws_bytes, hipStream_t stream) {
+  const TraceRange range("stepprune_compact_positions");
+  if (B < 1 || T_vis < 0 || T_txt < 0 || out_rows < 0 || axes < 1 || axes > 3) return SP_EINVAL;
+  if (layout != SP_LAYOUT_PADDED && layout != SP_LAYOUT_PACKED) return SP_EINVAL;
+  if (layout == SP_LAYOUT_PADDED && (rows_per_image < 0 || (int64_t)rows_per_image * B > out_rows))
+    return SP_EINVAL;
+  if ((T_vis > 0 && !vis_pos) || (T_txt > 0 && !text_pos) || (out_rows > 0 && !pos)) return SP_EINVAL;
+  if (!img_off || !text_off || !kept_idx || !kept_off || !kept_cnt || !ws || !aligned16(ws))
+    return SP_EINVAL;
+  if (ws_bytes < kWsHeaderBytes) return SP_EWORKSPACE;
+  PositionsArgs a;
+  a.vis_pos = vis_pos;
+  a.T_vis = T_vis;
+  a.img_off = img_off;
+  a.text_pos = text_pos;
+  a.T_txt = T_txt;
+  a.text_off = text_off;
+  a.axes = axes;
+  a.kept_idx = kept_idx;
+  a.kept_off = kept_off;
+  a.kept_cnt = kept_cnt;
+  a.B = B;
+  a.layout = layout;
+  a.rows_per_image = rows_per_image;
+  a.out_rows = out_rows;
+  a.pos = pos;
+  a.err = reinterpret_cast<int32_t*>(ws);
+  return hip_status(launch_compact_positions(a, stream));
+}
+
+sp_status stepprune_cache_append(const sp_cache_dims* dims, const void* Q, int64_t ldq,
+                                 const void* K, int64_t ldk, const void* V, int64_t ldv,
+                                 const sp_cache_rows* rows, const sp_cache_runs* runs,
+                                 const sp_cache_rotation* rot, void* Q_out, void* k_cache,
+                                 void* v_cache, void* ws, size_t ws_bytes, hipStream_t stream) {
+  const TraceRange range("stepprune_cache_append");
+  AppendArgs a;
+  sp_status st = check_cache_dims(dims, a.shape);
+  if (st == SP_OK) st = check_cache_runs(runs, a.shape, true, a.runs);
+  if (st == SP_OK) st = check_cache_rows(rows, a.shape, a.runs.count, true, a.rows);
+  if (st != SP_OK) return st;
+  const int e = a.shape.dtype == SP_F32 ? 4 : 2;
+  const int64_t q_cols = (int64_t)a.shape.q_heads * a.shape.head_dim;
+  const int64_t kv_cols = (int64_t)a.shape.kv_heads * a.shape.head_dim;
+  if (!k_cache || !v_cache || !ws || !Q != !Q_out) return SP_EINVAL;
+  if (a.rows.rows > 0 && (!K || !V)) return SP_EINVAL;
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(Q_out) || !aligned16(k_cache) ||
+      !aligned16(v_cache) || !aligned16(ws))
+    return SP_EINVAL;
+  if ((Q && (ldq < q_cols || ldq * e % 16)) || ldk < kv_cols || ldk * e % 16 || ldv < kv_cols || ldv * e % 16)
+    return SP_EINVAL;
+  if (Q && Q == Q_out && ldq != q_cols) return SP_EINVAL;
+  a.cos_sin = nullptr;
+  a.pos = nullptr;
+  a.positions = a.rot_dim = a.interleaved = a.sec1 = a.sec2 = 0;
+  a.axes = 1;
+  if (rot) {
+    if (!rot->cos_sin || !aligned16(rot->cos_sin) || rot->positions < 1) return SP_EINVAL;
+    if (rot->rot_dim < 16 || rot->rot_dim % 16 || rot->rot_dim > a.shape.head_dim) return SP_EINVAL;
+    if (rot->interleaved != 0 && rot->interleaved != 1) return SP_EINVAL;
+    if (rot->axes < 1 || rot->axes > (rot->pos ? 3 : 1)) return SP_EINVAL;
+    int64_t pairs = 0;
+    for (int i = 0; i < rot->axes; ++i) {
+      if (rot->section[i] < 0) return SP_EINVAL;
+      pairs += rot->section[i];
+    }
+    if (pairs != rot->rot_dim / 2) return SP_EINVAL;
+    a.cos_sin = rot->cos_sin;
+    a.pos = rot->pos;
+    a.positions = rot->positions;
+    a.rot_dim = rot->rot_dim;
+    a.interleaved = rot->interleaved;
+    a.axes = rot->axes;
+    a.sec1 = rot->axes > 1 ? rot->section[0] : (int)pairs;
+    a.sec2 = rot->axes > 2 ? rot->section[0] + rot->section[1] : (int)pairs;
+  }
+  if (ws_bytes < kWsHeaderBytes) return SP_EWORKSPACE;
+  a.Q = Q;
+  a.K = K;
+  a.V = V;
+  a.ldq = ldq;
+  a.ldk = ldk;
+  a.ldv = ldv;
+  a.Q_out = Q_out;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.err = reinterpret_cast<int32_t*>(ws);
+  return hip_status(launch_cache_append(a, stream));
+}
+
+size_t stepprune_cache_workspace_bytes(const sp_cache_dims* dims, const sp_cache_rows* rows,
+                                       const sp_cache_runs* runs, const sp_cache_runs* prefix) {
+  AttendArgs a;
+  if (check_attend(dims, rows, runs, prefix, false, a) != SP_OK) return 0;
+  return attend_ws_layout(a).total;
+}
+
+sp_status stepprune_cache_attend(const sp_cache_dims* dims, const void* Q, int64_t ldq,
+                                 const sp_cache_rows* rows, const sp_cache_runs* runs,
+                                 const sp_cache_runs* prefix, const int32_t* grp_off, float scale,
+                                 uint32_t flags, const void* k_cache, const void* v_cache, void* O,
+                                 float* lse, void* ws, size_t ws_bytes, const hipEvent_t* events,
+                                 hipStream_t stream) {
+  const TraceRange range("stepprune_cache_attend");
+  AttendArgs a;
+  const sp_status st = check_attend(dims, rows, runs, prefix, true, a);
+  if (st != SP_OK) return st;
+  if (flags & ~(uint32_t)SP_ATTEND_ALL) return SP_EINVAL;
+  // -inf, a masked score, stays -inf times the scale
+  const float c2 = scale * 1.4426950408889634f;
+  if (!(c2 >= FLT_MIN && c2 <= FLT_MAX)) return SP_EINVAL;
+  if (!k_cache || !v_cache || !ws || !prefix != !grp_off) return SP_EINVAL;
+  if (a.rows.rows > 0 && (!Q || !O || Q == O)) return SP_EINVAL;
+  if (!aligned16(Q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(O) || !aligned16(ws))
+    return SP_EINVAL;
+  if (ldq < (int64_t)a.shape.q_heads * a.shape.head_dim || ldq * (a.shape.dtype == SP_F32 ? 4 : 2) % 16)
+    return SP_EINVAL;
+  const AttendWs w = attend_ws_layout(a);
+  if (ws_bytes < w.total) return SP_EWORKSPACE;
+  char* base = static_cast<char*>(ws);
+  a.grp_off = grp_off;
+  a.Q = Q;
+  a.ldq = ldq;
+  a.c2 = c2;
+  a.all = (flags & SP_ATTEND_ALL) != 0;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.O = O;
+  a.lse = lse;
+  a.row_parts = reinterpret_cast<int32_t*>(base + w.row_parts);
+  a.part_ml = reinterpret_cast<float*>(base + w.ml);
+  a.part_o = reinterpret_cast<float*>(base + w.o);
+  a.err = reinterpret_cast<int32_t*>(base);
+  record_event(events, 0, stream);
+  const hipError_t e = launch_cache_attend(a, stream);
   record_event(events, 1, stream);
   return hip_status(e);
 }

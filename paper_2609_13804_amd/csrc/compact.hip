@@ -100,7 +100,71 @@ __global__ __launch_bounds__(kCompactWaves * 64) void compact_kernel(CompactArgs
   }
 }
 
+// The compaction of positions: row r of image b's sequence gets the position of
+// the token that compact_kernel puts there, on every axis.  Grid: row_blocks
+// workgroups to an image.  A few hundred kilobytes at most, so latency is all: every wave sums the
+// earlier images' kept counts by itself (no LDS, no barrier).
+constexpr int kPosThreads = 256;
+__global__ __launch_bounds__(kPosThreads) void positions_kernel(PositionsArgs p, int row_blocks) {
+  const int b = blockIdx.x / row_blocks, block = blockIdx.x % row_blocks, lane = threadIdx.x & 63;
+  const int64_t t0 = p.text_off[b], t1 = p.text_off[b + 1];
+  const int64_t i0 = p.img_off[b], i1 = p.img_off[b + 1];
+  const int64_t k0 = p.kept_off[b], k1 = p.kept_off[b + 1];
+  const int64_t K = p.kept_cnt[b];
+  const bool report = block == 0 && threadIdx.x == 0;
+  if (t0 < 0 || t1 < t0 || t1 > p.T_txt || i0 < 0 || i1 < i0 || i1 > p.T_vis || k1 < k0 || k0 < 0 || K < 0 ||
+      K > k1 - k0) {
+    if (report) set_device_error(p.err, SP_DEV_BAD_OFFSETS);
+    return;
+  }
+  const int64_t L = t1 - t0;
+  int64_t base;
+  if (p.layout == SP_LAYOUT_PADDED) {
+    base = (int64_t)b * p.rows_per_image;
+    if (K + L > p.rows_per_image) {
+      if (report) set_device_error(p.err, SP_DEV_OUTPUT_OVERFLOW);
+      return;
+    }
+  } else {
+    int64_t s = 0;
+    for (int i = lane; i < b; i += 64) s += p.kept_cnt[i];
+    for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m, 64);
+    base = s + (t0 - p.text_off[0]);
+  }
+  if (base < 0 || base + K + L > p.out_rows) {
+    if (report) set_device_error(p.err, SP_DEV_OUTPUT_OVERFLOW);
+    return;
+  }
+  for (int64_t r = (int64_t)block * kPosThreads + threadIdx.x; r < K + L;
+       r += (int64_t)row_blocks * kPosThreads) {
+    const int32_t* src;
+    int64_t ld;
+    if (r < K) {
+      const int64_t idx = p.kept_idx[k0 + r];
+      if (idx < 0 || idx >= i1 - i0) {
+        set_device_error(p.err, SP_DEV_BAD_OFFSETS);
+        continue;
+      }
+      src = p.vis_pos + i0 + idx;
+      ld = p.T_vis;
+    } else {
+      src = p.text_pos + t0 + r - K;
+      ld = p.T_txt;
+    }
+    for (int a = 0; a < p.axes; ++a) p.pos[a * p.out_rows + base + r] = src[a * ld];
+  }
+}
+
 }  // namespace
+
+hipError_t launch_compact_positions(const PositionsArgs& a, hipStream_t stream) {
+  const int64_t per_image = a.layout == SP_LAYOUT_PADDED ? a.rows_per_image : a.out_rows / a.B + 1;
+  int64_t x = (per_image + kPosThreads - 1) / kPosThreads;
+  if (x < 1) x = 1;
+  if (x > 32) x = 32;
+  hipLaunchKernelGGL(positions_kernel, dim3((unsigned)(x * a.B)), dim3(kPosThreads), 0, stream, a, (int)x);
+  return hipGetLastError();
+}
 
 hipError_t launch_compact(const CompactArgs& a, hipStream_t stream) {
   if (a.B == 0) return hipSuccess;

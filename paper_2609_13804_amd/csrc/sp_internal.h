@@ -144,6 +144,105 @@ struct CompactArgs {
 };
 hipError_t launch_compact(const CompactArgs& a, hipStream_t stream);
 
+// The compaction of positions: the same rows of int32 [axes] columns.
+struct PositionsArgs {
+  const int32_t* vis_pos;
+  int64_t T_vis;
+  const int32_t* img_off;
+  const int32_t* text_pos;
+  int64_t T_txt;
+  const int32_t* text_off;
+  int axes;
+  const int32_t* kept_idx;
+  const int32_t* kept_off;
+  const int32_t* kept_cnt;
+  int B;
+  int layout;
+  int rows_per_image;
+  int64_t out_rows;
+  int32_t* pos;
+  int32_t* err;
+};
+hipError_t launch_compact_positions(const PositionsArgs& a, hipStream_t stream);
+
+// The paged cache (stepprune.h's sp_cache_* structs, checked): cache.hip
+// appends, attend.hip reads.
+constexpr int kMaxCacheHeads = 1024;        // query heads
+constexpr int kMaxCacheRows = (1 << 26) - 1;// rows times query heads of a key head (a wave a row fits a grid)
+struct CacheShape {
+  int q_heads, kv_heads, head_dim, dtype;
+  int page_shift;         // log2 of page_size
+  int pages;
+};
+struct CacheRows {
+  int64_t rows;
+  int padded;
+  int rows_per_seq;
+  const int32_t* info;
+  int max_rows;
+};
+struct CacheRuns {
+  const int32_t* table;
+  const int32_t* len;
+  int count;
+  int width;
+  int max_len;
+};
+struct AppendArgs {
+  CacheShape shape;
+  CacheRows rows;
+  CacheRuns runs;
+  const void* Q;
+  const void* K;
+  const void* V;
+  int64_t ldq, ldk, ldv;
+  // rotation; cos_sin null: none
+  const float* cos_sin;
+  const int32_t* pos;
+  int positions, rot_dim, interleaved, axes;
+  int sec1, sec2;         // the first pair of axis 1, of axis 2
+  void* Q_out;
+  void* k_cache;
+  void* v_cache;
+  int per_wave;           // passes (of 64 lanes' heads) a wave makes over its row
+  int splits;             // waves to a row
+  int32_t* err;
+};
+hipError_t launch_cache_append(AppendArgs a, hipStream_t stream);
+
+// Attention's split of the work, from the bounds alone (attend.hip): query rows
+// times key heads in tiles, keys in chunks; a row's result over a chunk is a
+// part.
+struct AttendPlan {
+  int prefix_tall, own_tall;              // whether the tall tiles are launched
+  int chunk_prefix, chunk_thin, chunk_tall;
+  int prefix_parts, own_parts;            // most parts of a row
+};
+struct AttendArgs {
+  CacheShape shape;
+  CacheRows rows;
+  CacheRuns runs;
+  CacheRuns prefix;       // count 0: none
+  const int32_t* grp_off;
+  const void* Q;
+  int64_t ldq;
+  float c2;               // scale log2(e)
+  int all;                // every row sees its sequence's whole run
+  const void* k_cache;
+  const void* v_cache;
+  void* O;
+  float* lse;
+  AttendPlan plan;
+  // workspace pieces
+  int32_t* row_parts;     // [rows]
+  float* part_ml;         // [rows, q_heads, parts, 2]
+  float* part_o;          // [rows, q_heads, parts, head_dim]
+  int32_t* err;
+};
+AttendPlan plan_cache_attend(const CacheShape& shape, const CacheRows& rows, const CacheRuns& runs,
+                             const CacheRuns& prefix);
+hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t stream);
+
 // C = A B^T for bfloat16 A [M, K] and B [N, K] (rows K-contiguous), bfloat16
 // C [M, N]; K a multiple of 64.  With bias [N] (float32) each element is
 // bf16(bf16(product) + bias), or bf16(GELU(bf16(product) + bias)) with gelu:

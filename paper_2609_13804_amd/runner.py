@@ -194,6 +194,26 @@ class DeviceRun:
                                     self.seq_info, self.ws[2], self.ws_bytes[2], stream,
                                     events=events)
 
+    def positions(self, vis_pos, text_pos, pos=None, stream=None):
+        """Positions of the compacted buffer's rows, [axes, out_rows] int32, from the
+        tokens' own (``vis_pos`` [axes, T_vis], ``text_pos`` [axes, T_txt], int32 on the
+        device): what the rotation of their keys takes.  Zero where the buffer has no row."""
+        s = self.sizes
+        if pos is None:
+            pos = torch.zeros((vis_pos.shape[0], self.out_rows), dtype=torch.int32, device=self.X.device)
+        sp.stepprune_compact_positions(vis_pos, s.T_vis, self.img_off, text_pos, s.T_txt, self.text_off,
+                                       vis_pos.shape[0], self.kept_idx, self.kept_off, self.kept_cnt, s.B,
+                                       self.layout_code, self.rows_per_image, self.out_rows, pos,
+                                       self.ws[2], self.ws_bytes[2], stream)
+        return pos
+
+    def cache_rows(self, max_rows: Optional[int] = None):
+        """The compacted buffer's rows as the cache's calls take them (seq_info as
+        compact() leaves it)."""
+        most = self.rows_per_image if self.layout_code == sp.SP_LAYOUT_PADDED else self.out_rows
+        return sp.cache_rows(self.out_rows, self.layout_code, self.rows_per_image, self.seq_info,
+                             most if max_rows is None else max_rows)
+
     def run(self, stream=None):
         self.project(stream)
         self.select(stream)
