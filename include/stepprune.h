@@ -562,8 +562,9 @@ enum { SP_ATTEND_ALL = 1u };  /* every row sees its sequence's whole run */
  * j < L_s):
  *   o = sum_j softmax_j(scale <q, k_j>) v_j,   lse = log sum_j exp(scale <q, k_j>).
  * A row that sees no token (or only scores of -inf) gives o = 0, lse = -inf.
- * Tokens that a row does not see have no influence on it, whatever their pages
- * hold.  A prefix is read once for the rows of all its sequences.  With
+ * Tokens that a row does not see are no part of its sums, whatever their pages
+ * hold (infinite or NaN values of tokens that only later rows see change the
+ * order of the sums, so their rounding).  A prefix is read once for the rows of all its sequences.  With
  * prefixes and runs of length 0 this is cross attention to the prefixes.
  *
  *  Q        [rows, q_heads head_dim], row stride ldq; 16-byte aligned

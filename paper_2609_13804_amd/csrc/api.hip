@@ -171,19 +171,25 @@ sp_status check_attend(const sp_cache_dims* dims, const sp_cache_rows* rows, con
   return st;
 }
 
-// Header; parts of every row; the parts' maxima and sums, and their outputs,
-// [rows][q_heads][parts] (none where a row has one part at most, which is its output).
+// Header; parts of every row; the parts' maxima and sums, and their outputs (none where
+// a row has one part at most, which is its output).
 struct AttendWs {
-  size_t row_parts, ml, o, total;
+  size_t row_parts, ml[3], o[3], total;              // short, prefix, tall
 };
 AttendWs attend_ws_layout(const AttendArgs& a) {
+  const AttendPlan& p = a.plan;
+  const size_t brief = (size_t)a.runs.count * p.short_rows * a.shape.q_heads;
+  const bool joined = p.prefix_parts > 0 || p.short_parts > 1;
+  const size_t n[3] = {joined ? brief * p.short_parts : 0, brief * p.prefix_parts,
+                       p.tall_parts > 1 ? (size_t)a.rows.rows * a.shape.q_heads * p.tall_parts : 0};
   AttendWs w;
-  const size_t parts = (size_t)a.plan.prefix_parts + a.plan.own_parts;
-  const size_t n = parts > 1 || a.plan.prefix_parts ? (size_t)a.rows.rows * a.shape.q_heads * parts : 0;
   w.row_parts = kWsHeaderBytes;
-  w.ml = align_up(w.row_parts + (size_t)a.rows.rows * 4, 256);
-  w.o = align_up(w.ml + n * 2 * 4, 256);
-  w.total = align_up(w.o + n * a.shape.head_dim * 4, 256);
+  w.total = align_up(w.row_parts + (size_t)a.rows.rows * sizeof(int2), 256);
+  for (int i = 0; i < 3; ++i) {
+    w.ml[i] = w.total;
+    w.o[i] = align_up(w.ml[i] + n[i] * 2 * 4, 256);
+    w.total = align_up(w.o[i] + n[i] * a.shape.head_dim * 4, 256);
+  }
   return w;
 }
 
@@ -608,9 +614,13 @@ sp_status stepprune_cache_attend(const sp_cache_dims* dims, const void* Q, int64
   a.v_cache = v_cache;
   a.O = O;
   a.lse = lse;
-  a.row_parts = reinterpret_cast<int32_t*>(base + w.row_parts);
-  a.part_ml = reinterpret_cast<float*>(base + w.ml);
-  a.part_o = reinterpret_cast<float*>(base + w.o);
+  a.row_parts = reinterpret_cast<int2*>(base + w.row_parts);
+  a.short_ml = reinterpret_cast<float*>(base + w.ml[0]);
+  a.short_o = reinterpret_cast<float*>(base + w.o[0]);
+  a.prefix_ml = reinterpret_cast<float*>(base + w.ml[1]);
+  a.prefix_o = reinterpret_cast<float*>(base + w.o[1]);
+  a.tall_ml = reinterpret_cast<float*>(base + w.ml[2]);
+  a.tall_o = reinterpret_cast<float*>(base + w.o[2]);
   a.err = reinterpret_cast<int32_t*>(base);
   record_event(events, 0, stream);
   const hipError_t e = launch_cache_attend(a, stream);

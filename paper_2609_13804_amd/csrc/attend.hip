@@ -5,7 +5,7 @@
 // over the tokens of the row's prefix run (all of them) and of its own run (up
 // to the row's own place, or all).
 //
-// A tile is 32 or 128 consecutive (row, head) pairs of one segment and one key
+// A tile is 16 or 128 consecutive (row, head) pairs of one segment and one key
 // head: a segment is a sequence's rows, over its own run, or the rows of all
 // the sequences of a group, over the group's prefix, which is so read once for
 // all of them.  Pair x of a segment is row x / r, head x % r of the key head's r
@@ -15,7 +15,16 @@
 // 2^(s - m) (scores s in powers of two).  A row with a single part is done; the
 // others' parts go to the workspace and combine_kernel joins them:
 //   o = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p,  M = max_p m_p.
+//
+// A sequence's pairs to a key head decide what its rows run in:
+//   up to 16          thin tiles (memory-bound: the waves split the keys)
+//   more              tall tiles (the waves split the pairs)
+//   more than kFuse   tall tiles that take the prefix's keys first and then its own:
+//                     such a sequence fills tiles by itself, so sharing the prefix's
+//                     reads saves nothing and parts would only be written and read.
 #include <float.h>
+
+#include <type_traits>
 
 #include "sp_internal.h"
 #include "cache_rows.h"
@@ -28,12 +37,14 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) bf16x4_t* ltr_t;
 
-constexpr int kThin = 32, kTall = 128;     // pairs of a tile
-constexpr int kThinF32 = 16;
+constexpr int kThin = 16, kTall = 128;     // pairs of a tile
+constexpr int kFuse = 64;                  // pairs of a sequence past which it takes its prefix by itself
 constexpr int kWaves = 4;
-constexpr int kThinStep = 32 * kWaves;     // keys that the waves of a thin tile take together
+constexpr int kMaxParts = 1024;
+constexpr int kThinStep = 16 * kWaves;     // keys that the waves of a thin tile take together
 constexpr int kTallStep = 64;
 // Running maxima start here: a masked score (-inf) then weighs 2^-inf = 0 also
 // where a row has seen nothing yet.
@@ -109,37 +120,151 @@ __device__ __forceinline__ void report_entries(const AttendArgs& a, bool prefix)
   }
 }
 
-// Tokens that pair x sees of the segment's run.
+// Tokens of the segment's run that its row `row` sees.
 __device__ __forceinline__ int sees(const AttendArgs& a, const Tile& t, bool prefix, int row) {
   if (prefix || a.all) return t.len;
   const int64_t v = (int64_t)t.len - t.n + row + 1;
   return v < 0 ? 0 : (int)v;
 }
 
-// Parts of a row's prefix: 0 without one.
-__device__ __forceinline__ int prefix_parts(const AttendArgs& a, int s) {
+// The group of sequence s and the tokens of its prefix: 0 without one.
+__device__ __forceinline__ int prefix_of(const AttendArgs& a, int s, int& g) {
+  g = 0;
   if (a.prefix.count == 0) return 0;
-  const int g = wave_find_last(a.prefix.count, s, [&](int i) { return a.grp_off[i]; });
+  g = wave_find_last(a.prefix.count, s, [&](int i) { return a.grp_off[i]; });
   int len;
   if (s < a.grp_off[g] || s >= a.grp_off[g + 1] || tokens_of(a.prefix, g, len) != SP_DEV_OK) return 0;
-  return (len + a.plan.chunk_prefix - 1) / a.plan.chunk_prefix;
+  return len;
 }
 
-// A run's pages by block of 16 tokens, 64 blocks at a time in a wave's lanes.
-struct Pages {
+__device__ __forceinline__ int ceil_div(int x, int y) { return (x + y - 1) / y; }
+
+// A run's pages from page `base` on, 64 in a wave's lanes and the next 64 on their way.
+struct Window {
   const int32_t* table;
-  int shift, count, blocks;    // log2 of blocks of a page; pages of the cache; blocks of the run
-  __device__ __forceinline__ int load(int block0, int32_t* err) const {
-    const int b = block0 + (int)(threadIdx.x & 63);
-    int p = 0;
-    if (b < blocks) p = table[b >> shift];
+  int used, count;             // pages of the run, of the cache
+  int base, now, next;
+  __device__ __forceinline__ int fetch(int p0, int32_t* err) const {
+    const int i = p0 + (int)(threadIdx.x & 63);
+    int p = i < used ? table[i] : 0;
     if ((uint32_t)p >= (uint32_t)count) {
       set_device_error(err, SP_DEV_BAD_PAGE);
       p = 0;
     }
     return p;
   }
+  __device__ __forceinline__ void start(const AttendArgs& a, const int32_t* pages, int tokens, int key0) {
+    table = pages;
+    used = ceil_div(tokens, 1 << a.shape.page_shift);
+    count = a.shape.pages;
+    const int p0 = key0 >> a.shape.page_shift;
+    int32_t* const err = a.err;
+    base = p0;
+    now = fetch(p0, err);
+    next = fetch(p0 + 64, err);
+  }
+  // page i of the run, i >= base, in steps of at most 64
+  __device__ __forceinline__ int page(int i, int32_t* err) {
+    if (i - base >= 64) {
+      base += 64;
+      now = next;
+      next = fetch(base + 64, err);
+    }
+    return __builtin_amdgcn_readlane(now, i - base);
+  }
 };
+
+// An address that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ const char* uniform(const char* p) {
+  const uint64_t u = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
+  return reinterpret_cast<const char*>(((uint64_t)hi << 32) | lo);
+}
+
+// ---- where a pair's result goes
+
+struct Out {
+  int64_t pair;           // row q_heads + head; -1: nowhere
+  bool done;              // the only part: into O; else a part, at
+  float* o;
+  float2* ml;
+};
+
+// Sequences of up to this many pairs are short: their parts lie by sequence.
+__device__ __forceinline__ bool is_short(const AttendArgs& a, int pairs) { return pairs <= a.plan.short_pairs; }
+
+__device__ __forceinline__ int64_t short_base(const AttendArgs& a, int s, int row_of_seq) {
+  return ((int64_t)s * a.plan.short_rows + row_of_seq) * a.shape.q_heads;
+}
+
+// Pair x of sequence t.seg and key head h: the place of its result over chunk `chunk` of
+// the `own` chunks of its own keys, with `pre` parts of its prefix beside them.  First
+// chunk: the row's parts, for combine_kernel.
+__device__ __forceinline__ Out own_place(const AttendArgs& a, const Tile& t, int h, int x, int chunk, int own, int pre) {
+  Out u;
+  u.pair = -1;
+  u.done = pre == 0 && own <= 1;                     // (a row that sees nothing: zeros, by its first chunk)
+  const int r = ratio(a), i = x / r, head = h * r + (x - i * r);
+  const int64_t row = t.row0 + i;
+  if (chunk == 0 && h == 0 && x == i * r) a.row_parts[row] = make_int2(u.done ? 0 : own, pre);
+  if (chunk >= own && !(u.done && chunk == 0)) return u;
+  u.pair = row * a.shape.q_heads + head;
+  int64_t at;
+  if (is_short(a, t.pairs)) {
+    at = (short_base(a, t.seg, i) + head) * a.plan.short_parts + chunk;
+    u.o = a.short_o;
+    u.ml = reinterpret_cast<float2*>(a.short_ml);
+  } else {
+    at = u.pair * a.plan.tall_parts + chunk;
+    u.o = a.tall_o;
+    u.ml = reinterpret_cast<float2*>(a.tall_ml);
+  }
+  u.o += at * a.shape.head_dim;
+  u.ml += at;
+  return u;
+}
+
+// The same for pair x of group t.seg over a chunk of the group's prefix.  Nowhere: a padded
+// slice's rows past its count, and the rows of a sequence that takes the prefix by itself.
+__device__ __forceinline__ Out prefix_place(const AttendArgs& a, const Tile& t, int h, int x, int chunk) {
+  Out u;
+  u.pair = -1;
+  u.done = false;
+  const int r = ratio(a), j = x / r, head = h * r + (x - j * r);
+  const int64_t row = t.row0 + j;
+  int s, i, n;
+  if (a.rows.padded) {
+    s = (int)(row / a.rows.rows_per_seq);
+    i = (int)(row - (int64_t)s * a.rows.rows_per_seq);
+    n = a.rows.info[s];
+  } else {                                           // info[s] <= row < info[s + 1]
+    s = a.grp_off[t.seg];
+    for (int hi = a.grp_off[t.seg + 1]; hi - s > 1;) {
+      const int mid = (s + hi) >> 1;
+      if (a.rows.info[mid] <= row) s = mid;
+      else hi = mid;
+    }
+    const int first = a.rows.info[s];
+    i = (int)(row - first);
+    n = a.rows.info[s + 1] - first;
+  }
+  if (i < 0 || i >= n || n > a.rows.max_rows || (int64_t)n * r > a.plan.short_pairs) return u;
+  u.pair = row * a.shape.q_heads + head;
+  const int64_t at = (short_base(a, s, i) + head) * a.plan.prefix_parts + chunk;
+  u.o = a.prefix_o + at * a.shape.head_dim;
+  u.ml = reinterpret_cast<float2*>(a.prefix_ml) + at;
+  return u;
+}
+
+__device__ __forceinline__ float lse_of(float m, float l) {
+  return l > 0.0f || l != l ? (m + __log2f(l)) * 0.6931471805599453f : -INFINITY;
+}
+
+__device__ __forceinline__ void store_ml(const AttendArgs& a, const Out& u, float m, float l) {
+  if (!u.done) *u.ml = make_float2(m, l);
+  else if (a.lse) a.lse[u.pair] = lse_of(m, l);
+}
 
 // ---------------------------------------------------------------- bfloat16
 
@@ -151,336 +276,195 @@ __device__ __forceinline__ float half_sum(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+__device__ __forceinline__ float quad_max(float v) {      // of the four lanes 16 apart
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return half_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return half_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
 
 // A head's rows in LDS: ROW bytes each, 16-byte chunks swizzled so that a pass of a
-// fragment read touches every bank once: K (32 rows, a chunk of each) by the row,
-// V (four rows, 64 bytes of each) by the row on 64-byte pieces.
+// fragment read touches every bank once: K (a chunk of each of 16 or 32 rows) by the
+// row, V (64 bytes of each of four rows) by the row on 64-byte pieces.
 template <int D>
 struct Geo {
   static constexpr int ROW = 2 * D, CHUNKS = ROW / 16, LOAD_ROWS = 1024 / ROW;   // rows of a load
-  static constexpr int BLOCK = 32 * ROW;                                          // 32 keys
-  static constexpr int LOADS = BLOCK / 1024;
+  static constexpr int LOADS = 16 / LOAD_ROWS;                                    // loads of 16 keys
   __device__ static __forceinline__ int kswz(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
   __device__ static __forceinline__ int vswz(int r) { return D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; }
 };
 
-// One wave's 32 pairs: lane l holds pair l % 32; of 32 keys' scores those of keys
-// 8 (i / 4) + 4 (l / 32) + i % 4 in register i, and of the output elements
-// 32 t + 8 (i / 4) + 4 (l / 32) + i % 4 in o[t][i] (v_mfma_f32_32x32x16_bf16 with
-// keys, then values, as the row operand).
+// The loads of 16 keys (of one page) into LDS rows of K or of V: an instruction fills
+// 1 KB, lane i lands on chunk i % CHUNKS of row i / CHUNKS and fetches the chunk that
+// the swizzle puts there.  Keys from the run's end on are zeros.
 template <int D>
-struct Pairs {
-  bf16x8_t q[D / 16];
-  f32x16_t o[D / 32];
-  float m, l;             // m is the pair's, l this lane's share
-  int lim;                // tokens that the pair sees
-  int lim0;               // and the first pair of the wave
-};
-
-template <int D>
-__device__ __forceinline__ void init_pairs(Pairs<D>& w) {
-#pragma unroll
-  for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) w.o[t][i] = 0.0f;
-  w.m = kLowest;
-  w.l = 0.0f;
-}
-
-// Loads the wave's queries; x is this lane's pair.  Pairs past the segment are zero.
-template <int D>
-__device__ __forceinline__ void load_queries(const AttendArgs& a, const Tile& t, bool prefix, int h, int x,
-                                             int x_first, Pairs<D>& w) {
-  const int half = (threadIdx.x & 63) >> 5, r = ratio(a);
-  const bool live = x < t.pairs;
-  const int row = live ? x / r : 0, sub = x - row * r;
-  const uint16_t* src = static_cast<const uint16_t*>(a.Q) + (t.row0 + row) * a.ldq + (h * r + sub) * D;
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
-    uint4 u = make_uint4(0, 0, 0, 0);
-    if (live) u = *reinterpret_cast<const uint4*>(src + 16 * s + 8 * half);
-    w.q[s] = __builtin_bit_cast(bf16x8_t, u);
-  }
-  w.lim = live ? sees(a, t, prefix, row) : 0;
-  w.lim0 = x_first < t.pairs ? sees(a, t, prefix, x_first / r) : 0;
-}
-
-template <int D>
-__device__ __forceinline__ bf16x4_t read_vt(const char* V, int t, int row0) {
-  const int lane = threadIdx.x & 63, vr = (lane >> 2) & 3, row = row0 + 4 * (lane >> 5) + vr;
-  const int piece = 4 * t ^ Geo<D>::vswz(vr);             // (row0 + 4 half is a multiple of 4)
-  return __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-      (ltr_t)(V + row * Geo<D>::ROW + piece * 16 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8));
-}
-
-// 32 NB keys from key kb on, in the LDS tiles K and V, whose rows hold zeros from key
-// `loaded` on.  values() returns once V is there.
-template <int D, int NB, typename Wait>
-__device__ __forceinline__ void step(Pairs<D>& w, const char* K, const char* V, int kb, int loaded,
-                                     float c2, Wait values) {
+struct Loader {
   using G = Geo<D>;
-  const int lane = threadIdx.x & 63, ql = lane & 31, half = lane >> 5;
-  f32x16_t st[NB];
+  const char* K;               // the key head's part of page 0
+  const char* V;
+  int64_t page_bytes;
+  int shift, page_mask, lr;
+  uint32_t ko[G::LOADS], vo;
+  __device__ __forceinline__ void init(const AttendArgs& a, int h) {
+    shift = a.shape.page_shift;
+    page_mask = (1 << shift) - 1;
+    page_bytes = (int64_t)a.shape.kv_heads * G::ROW << shift;
+    K = static_cast<const char*>(a.k_cache) + ((int64_t)h * G::ROW << shift);
+    V = static_cast<const char*>(a.v_cache) + ((int64_t)h * G::ROW << shift);
+    const int lane = threadIdx.x & 63, ch = lane % G::CHUNKS;
+    lr = lane / G::CHUNKS;
 #pragma unroll
-  for (int n = 0; n < NB; ++n)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) st[n][i] = 0.0f;
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s)
-#pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      const uint4 u = *reinterpret_cast<const uint4*>(K + n * G::BLOCK + ql * G::ROW +
-                                                      (((2 * s + half) ^ G::kswz(ql)) << 4));
-      st[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, u), w.q[s], st[n], 0, 0, 0);
-    }
-  const bool masked = kb + 32 * NB > w.lim0;
-  if (masked) {
-#pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (kb + 32 * n + 8 * (i >> 2) + 4 * half + (i & 3) >= w.lim) st[n][i] = -INFINITY;
+    for (int g = 0; g < G::LOADS; ++g)
+      ko[g] = g * 1024 + lr * G::ROW + ((ch ^ G::kswz(G::LOAD_ROWS * g + lr)) << 4);
+    vo = lr * G::ROW + ((ch ^ G::vswz(lr)) << 4);
   }
-  float bm = st[0][0];
+  template <bool VALUES>
+  __device__ __forceinline__ void load(int page, int key0, int end, char* dst) const {
+    const char* src = uniform((VALUES ? V : K) + page * page_bytes + (int64_t)(key0 & page_mask) * G::ROW);
+    if (key0 + 16 <= end) {
 #pragma unroll
-  for (int n = 0; n < NB; ++n)
+      for (int g = 0; g < G::LOADS; ++g) lds_dma16(src, VALUES ? vo + g * 1024 : ko[g], dst + g * 1024);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) bm = fmaxf(bm, st[n][i]);
-  const float mx = half_max(bm) * c2;
-  if (__any(mx > w.m + kRescale)) {
-    const float mn = fmaxf(w.m, mx);
-    const float sc = __builtin_amdgcn_exp2f(w.m - mn);
-    w.m = mn;
-    w.l *= sc;
-#pragma unroll
-    for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) w.o[t][i] *= sc;
-  }
-#pragma unroll
-  for (int n = 0; n < NB; ++n)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      st[n][i] = __builtin_amdgcn_exp2f(fmaf(st[n][i], c2, -w.m));
-      w.l += st[n][i];
-    }
-  values();
-  // Keys that some pairs see and others do not: a product would weigh them with 0
-  // for the others, which is NaN where the value is infinite or NaN.  Such tiles
-  // (never in sound data) go key by key.
-  if (masked && min(kb + 32 * NB, loaded) > w.lim0) {
-    uint32_t bad = 0;
-#pragma unroll
-    for (int c = 0; c < NB * G::LOADS; ++c) {
-      const uint4 u = *reinterpret_cast<const uint4*>(V + c * 1024 + lane * 16);
-      const uint32_t v[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        bad |= (uint32_t)((v[k] & 0x7f800000u) == 0x7f800000u) | (uint32_t)((v[k] & 0x7f80u) == 0x7f80u);
-    }
-    if (__any(bad)) {
-      for (int n = 0; n < NB; ++n)
-        for (int i = 0; i < 16; ++i) {
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            const float p = (float)(__bf16)__shfl(st[0][0], ql + 32 * hf, 64);
-            const int key = 32 * n + 8 * (i >> 2) + 4 * hf + (i & 3);
-            if (kb + key < w.lim) {
-#pragma unroll
-              for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                  const bf16x4_t v = *reinterpret_cast<const bf16x4_t*>(
-                      V + key * G::ROW + (((4 * t + g) ^ G::vswz(key)) << 4) + 8 * half);
-#pragma unroll
-                  for (int k = 0; k < 4; ++k) w.o[t][4 * g + k] = fmaf(p, (float)v[k], w.o[t][4 * g + k]);
-                }
-            }
-          }
-          // the next key's probability into st[0][0]: registers have no index
-#pragma unroll
-          for (int k = 0; k < 16 * NB - 1; ++k) st[k >> 4][k & 15] = st[(k + 1) >> 4][(k + 1) & 15];
-        }
-      return;
-    }
-  }
-#pragma unroll
-  for (int n = 0; n < NB; ++n) {
-    bf16x8_t pb[2];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) pb[i >> 3][i & 7] = (__bf16)st[n][i];
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-      for (int t = 0; t < D / 32; ++t) {
-        const bf16x4_t lo = read_vt<D>(V, t, 32 * n + 16 * g), hi = read_vt<D>(V, t, 32 * n + 16 * g + 8);
-        const bf16x8_t v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        w.o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pb[g], w.o[t], 0, 0, 0);
+      for (int g = 0; g < G::LOADS; ++g) {
+        const bool in = key0 + G::LOAD_ROWS * g + lr < end;
+        lds_dma16(in ? (const void*)(src + (VALUES ? vo + g * 1024 : ko[g])) : (const void*)zeros16, dst + g * 1024);
       }
+    }
   }
-}
-
-// An address that is the same in all lanes, in scalar registers.
-__device__ __forceinline__ const char* uniform(const char* p) {
-  const uint64_t u = (uint64_t)p;
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u);
-  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
-  return reinterpret_cast<const char*>(((uint64_t)hi << 32) | lo);
-}
-
-// Loads LOAD_ROWS keys from key0 on (one page) into rows row0 .. of a tile of K and of V: an
-// instruction fills 1 KB, lane i lands on chunk i % CHUNKS of row i / CHUNKS and
-// fetches the chunk that the swizzle puts there.  Keys from `end` on are zeros.
-template <int D>
-__device__ __forceinline__ void load_group(const char* Kc, const char* Vc, int64_t head_page, int page_mask,
-                                           int key0, int row0, int end, char* K, char* V) {
-  using G = Geo<D>;
-  const int lane = threadIdx.x & 63, lr = lane / G::CHUNKS, ch = lane % G::CHUNKS;
-  const int64_t at = (head_page * (page_mask + 1) + (key0 & page_mask)) * G::ROW;   // uniform
-  const uint32_t ko = lr * G::ROW + ((ch ^ G::kswz(row0 + lr)) << 4);
-  const uint32_t vo = lr * G::ROW + ((ch ^ G::vswz(lr)) << 4);
-  if (key0 + G::LOAD_ROWS <= end) {
-    lds_dma16(uniform(Kc + at), ko, K + row0 * G::ROW);
-    lds_dma16(uniform(Vc + at), vo, V + row0 * G::ROW);
-  } else {
-    const bool in = key0 + lr < end;
-    lds_dma16(in ? (const void*)(Kc + at + ko) : (const void*)zeros16, K + row0 * G::ROW);
-    lds_dma16(in ? (const void*)(Vc + at + vo) : (const void*)zeros16, V + row0 * G::ROW);
-  }
-}
-
-// ---- where a pair's result goes
-
-struct Out {
-  int64_t row;            // -1: nowhere
-  int head;
-  bool done;              // the only part: into O; else a part
-  int part, parts;
 };
 
-// The pair's place and whether this part is its only one (own: parts of its
-// prefix pp).  First chunk: the row's count of parts, for combine_kernel.
-__device__ __forceinline__ Out place_of(const AttendArgs& a, const Tile& t, bool prefix, int h, int x, int chunk_keys,
-                                        int chunk, int pp) {
-  Out u;
-  const int r = ratio(a);
-  u.parts = a.plan.prefix_parts + a.plan.own_parts;
-  u.row = -1;
-  u.done = false;
-  u.part = prefix ? chunk : a.plan.prefix_parts + chunk;
-  u.head = 0;
-  if (x >= t.pairs) return u;
-  const int i = x / r;
-  const int64_t row = t.row0 + i;
-  u.head = h * r + (x - i * r);
-  if (prefix) {
-    // a padded slice's rows past its count
-    if (a.rows.padded && (int)(row % a.rows.rows_per_seq) >= a.rows.info[row / a.rows.rows_per_seq]) return u;
-    u.row = row;
-    return u;
+// Whether `rows` rows of V hold a value that is infinite or NaN.
+template <int D>
+__device__ __forceinline__ bool any_unsound(const char* V, int rows) {
+  bool bad = false;
+#pragma unroll 1
+  for (int c = threadIdx.x & 63; c < rows * Geo<D>::CHUNKS; c += 64) {
+    const uint4 u = *reinterpret_cast<const uint4*>(V + c * 16);
+    const uint32_t v[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) bad |= (v[k] & 0x7f800000u) == 0x7f800000u || (v[k] & 0x7f80u) == 0x7f80u;
   }
-  const int own = (sees(a, t, false, i) + chunk_keys - 1) / chunk_keys;
-  if (chunk == 0 && h == 0 && x == i * r) a.row_parts[row] = pp == 0 && own <= 1 ? 0 : (own | pp << 16);
-  u.done = pp == 0 && own <= 1;                      // (a row that sees nothing: zeros, by its first chunk)
-  if (chunk < own || (u.done && chunk == 0)) u.row = row;
-  return u;
+  return __any(bad);
 }
 
-__device__ __forceinline__ float lse_of(float m, float l) {
-  return l > 0.0f || l != l ? (m + __log2f(l)) * 0.6931471805599453f : -INFINITY;
-}
-
-__device__ __forceinline__ void store_ml(const AttendArgs& a, const Out& u, float m, float l) {
-  const int64_t pair = u.row * a.shape.q_heads + u.head;
-  if (u.done) {
-    if (a.lse) a.lse[pair] = lse_of(m, l);
-  } else {
-    reinterpret_cast<float2*>(a.part_ml)[pair * u.parts + u.part] = make_float2(m, l);
+// In a tile, a key that some pairs see and others do not is weighed with 0 for those,
+// which is NaN where its value is infinite or NaN.  A wave that meets one begins again
+// here, key by key, each pair over the keys that it sees alone (a hundred times slower,
+// and never needed by sound data).  Lane l holds pair l % PAIRS; with p = l / PAIRS of P
+// lanes a pair, elements 8 P s + 8 p + 0 .. 7 of its query in q[s] and 4 P g + 4 p + 0 .. 3
+// of its output in o[g].
+template <int D, int PAIRS>
+struct KeyByKey {
+  static constexpr int P = 64 / PAIRS;
+  f32x4_t o[D / (4 * P)];
+  float m, l;
+  __device__ __forceinline__ void start() {
+#pragma unroll
+    for (int g = 0; g < D / (4 * P); ++g) o[g] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    m = kLowest;
+    l = 0.0f;
   }
-}
+  __device__ __forceinline__ void add(const AttendArgs& a, const Loader<D>& ld, const int32_t* table,
+                                      const bf16x8_t (&q)[D / (8 * P)], int from, int to, int lim) {
+    const int p = (threadIdx.x & 63) / PAIRS;
+#pragma unroll 1
+    for (int key = from; key < to; ++key) {
+      int page = table[key >> ld.shift];
+      if ((uint32_t)page >= (uint32_t)a.shape.pages) page = 0;
+      const int64_t at = page * ld.page_bytes + (int64_t)(key & ld.page_mask) * Geo<D>::ROW;
+      float dot = 0.0f;
+#pragma unroll
+      for (int s = 0; s < D / (8 * P); ++s) {
+        const bf16x8_t k = *reinterpret_cast<const bf16x8_t*>(ld.K + at + 2 * (8 * P * s + 8 * p));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dot = fmaf((float)q[s][j], (float)k[j], dot);
+      }
+      const float sc = (P == 2 ? half_sum(dot) : quad_sum(dot)) * a.c2;
+      if (key < lim) {
+        const float mn = fmaxf(m, sc), f = __builtin_amdgcn_exp2f(m - mn), w = __builtin_amdgcn_exp2f(sc - mn);
+        m = mn;
+        l = fmaf(l, f, w);
+        const float wb = (float)(__bf16)w;
+#pragma unroll
+        for (int g = 0; g < D / (4 * P); ++g) {
+          const bf16x4_t v = *reinterpret_cast<const bf16x4_t*>(ld.V + at + 2 * (4 * P * g + 4 * p));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[g][k] = fmaf(wb, (float)v[k], o[g][k] * f);
+        }
+      }
+    }
+  }
+};
+
+constexpr int kAttendLds = 64 * 1024;      // two workgroups to a compute unit
 
 // ---------------------------------------------------------------- the thin tiles
 
-// 32 pairs; each of four waves takes every fourth block of 32 keys, through a ring
-// of its own in LDS (no barrier until the end), and the waves' results are
-// joined through LDS.
+// 16 pairs; each of four waves takes every fourth block of 16 keys through a ring of its
+// own in LDS (no barrier until the end), and the waves' results are joined through
+// LDS.  Scores S^T = K Q^T and O^T += V^T P as in the tall tiles, with 16 x 16
+// matrices: lane l holds pair l % 16, scores of keys 4 (l / 16) + i, output elements
+// 16 t + 4 (l / 16) + i.
 template <int D>
 struct ThinShape {
-  static constexpr int STAGES = D == 128 ? 2 : 4;
-  static constexpr int RING = STAGES * 2 * Geo<D>::BLOCK;
+  static constexpr int BLOCK = 16 * Geo<D>::ROW;                // 16 keys of K or V
+  static constexpr int STAGES = kAttendLds / (kWaves * 2 * BLOCK);
   static constexpr int PART_ROW = D + 4;
-  static constexpr int PARTS = kWaves * 32 * (PART_ROW + 2) * 4;
-  static constexpr int LDS = kWaves * RING > PARTS ? kWaves * RING : PARTS;
+  static_assert(kWaves * kThin * (PART_ROW + 2) * 4 <= kAttendLds, "the waves' results fit the rings");
 };
 
 template <int D>
-__global__ __launch_bounds__(64 * kWaves, 1) void thin_kernel(AttendArgs a, int prefix, int tiled) {
+__device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool prefix, const Tile& t, int h, int chunk) {
   using G = Geo<D>;
   using SH = ThinShape<D>;
-  __shared__ __attribute__((aligned(1024))) char smem[SH::LDS];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31;
-  const int h = blockIdx.y, chunk = blockIdx.z;
-  if (blockIdx.x == 0 && h == 0 && chunk == 0) report_entries(a, prefix);
-  Tile t;
-  if (tiled) {
-    if (!find_tile<kThin>(a, prefix, blockIdx.x, t)) return;
-  } else {                                           // a sequence to a tile; longer ones are the tall tiles'
-    t.seg = blockIdx.x;
-    if (rows_of(a.rows, t.seg, t.row0, t.n) != SP_DEV_OK) return;
-    const int64_t pairs = (int64_t)t.n * ratio(a);
-    if (pairs == 0 || pairs > kThin || tokens_of(a.runs, t.seg, t.len) != SP_DEV_OK) return;
-    t.pairs = (int)pairs;
-    t.x0 = 0;
-    t.table = a.runs.table + (int64_t)t.seg * a.runs.width;
-  }
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int ql = lane & 15, quad = lane >> 4, r = ratio(a);
   const int chunk_keys = prefix ? a.plan.chunk_prefix : a.plan.chunk_thin;
-  const int pp = prefix ? 0 : prefix_parts(a, t.seg);
+  int g;
+  const int pre = prefix ? 0 : ceil_div(prefix_of(a, t.seg, g), a.plan.chunk_prefix);
   // the last pair's limit is the tile's
-  const int last = min(t.x0 + kThin, t.pairs) - 1;
-  const int tile_end = sees(a, t, prefix, last / ratio(a));
+  const int tile_end = sees(a, t, prefix, (min(t.x0 + kThin, t.pairs) - 1) / r);
   const int k0 = chunk * chunk_keys;
   if (k0 >= tile_end && (prefix || chunk > 0)) return;
   const int k1 = min(tile_end, k0 + chunk_keys);
 
-  Pairs<D> w;
-  init_pairs(w);
-  load_queries<D>(a, t, prefix, h, t.x0 + ql, t.x0, w);
+  const int x = t.x0 + ql;
+  const bool live = x < t.pairs;
+  const int row = live ? x / r : 0;
+  const uint16_t* qsrc =
+      static_cast<const uint16_t*>(a.Q) + (t.row0 + row) * a.ldq + (h * r + (x - row * r)) * D + 8 * quad;
+  bf16x8_t q[D / 32];
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s) {
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (live) u = *reinterpret_cast<const uint4*>(qsrc + 32 * s);
+    q[s] = __builtin_bit_cast(bf16x8_t, u);
+  }
+  const int lim = live ? sees(a, t, prefix, row) : 0, lim0 = sees(a, t, prefix, t.x0 / r);
 
-  const int page_mask = (1 << a.shape.page_shift) - 1;
-  const Pages pages{t.table, a.shape.page_shift - 4, a.shape.pages, (t.len + 15) >> 4};
-  const char* Kc = static_cast<const char*>(a.k_cache);
-  const char* Vc = static_cast<const char*>(a.v_cache);
-  char* ring = smem + wave * SH::RING;
-  // block i of the wave: keys k0 + 32 (wave + 4 i); its two 16-key pages in lane i % 64's registers
-  const int blocks = k1 - k0 > 32 * wave ? (k1 - k0 - 32 * wave + kThinStep - 1) / kThinStep : 0;
-  int pg[2] = {0, 0};
-  auto fetch_pages = [&](int i0) {
-    const int b = (k0 >> 4) + 2 * (wave + kWaves * (i0 + lane));
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      int p = 0;
-      if (b + e < pages.blocks) p = pages.table[(b + e) >> pages.shift];
-      if ((uint32_t)p >= (uint32_t)pages.count) {
-        set_device_error(a.err, SP_DEV_BAD_PAGE);
-        p = 0;
-      }
-      pg[e] = p;
-    }
-  };
+  Loader<D> ld;
+  ld.init(a, h);
+  char* ring = smem + wave * SH::STAGES * 2 * SH::BLOCK;
+  // block i of the wave: 16 keys from k0 + 16 (wave + 4 i) on
+  const int blocks = k1 - k0 > 16 * wave ? (k1 - k0 - 16 * wave + kThinStep - 1) / kThinStep : 0;
+  Window win;
+  if (blocks > 0) win.start(a, t.table, t.len, k0 + 16 * wave);
   auto issue = [&](int i) {
-    if ((i & 63) == 0) fetch_pages(i);
-    const int kb = k0 + 32 * (wave + kWaves * i);
-    char* K = ring + (i % SH::STAGES) * 2 * G::BLOCK;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int64_t head_page = (int64_t)__builtin_amdgcn_readlane(pg[e], i & 63) * a.shape.kv_heads + h;
-#pragma unroll
-      for (int g = 0; g < G::LOADS / 2; ++g) {
-        const int row0 = 16 * e + G::LOAD_ROWS * g;
-        load_group<D>(Kc, Vc, head_page, page_mask, kb + row0, row0, k1, K, K + G::BLOCK);
-      }
-    }
+    const int key0 = k0 + 16 * (wave + kWaves * i);
+    char* dst = ring + (i % SH::STAGES) * 2 * SH::BLOCK;
+    const int page = win.page(key0 >> ld.shift, a.err);
+    ld.template load<false>(page, key0, k1, dst);
+    ld.template load<true>(page, key0, k1, dst + SH::BLOCK);
   };
+  f32x4_t o[D / 16];
+#pragma unroll
+  for (int e = 0; e < D / 16; ++e) o[e] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  float m = kLowest, l = 0.0f;
+  bool unsound = false;
+  const float c2 = a.c2;
 #pragma unroll
   for (int i = 0; i < SH::STAGES - 1; ++i)
     if (i < blocks) issue(i);
@@ -492,150 +476,401 @@ __global__ __launch_bounds__(64 * kWaves, 1) void thin_kernel(AttendArgs a, int 
     } else {
       wait_vmcnt<0>();
     }
-    // (the wait alone does not keep the compiler from moving reads of LDS over it)
+    // (a wait alone does not keep the compiler from moving reads of LDS over it)
     asm volatile("" ::: "memory");
-    const char* K = ring + (i % SH::STAGES) * 2 * G::BLOCK;
-    step<D, 1>(w, K, K + G::BLOCK, k0 + 32 * (wave + kWaves * i), k1, a.c2, [] {});
+    const int kb = k0 + 16 * (wave + kWaves * i);
+    const char* K = ring + (i % SH::STAGES) * 2 * SH::BLOCK;
+    const char* V = K + SH::BLOCK;
+    f32x4_t st = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) {
+      const uint4 u = *reinterpret_cast<const uint4*>(K + ql * G::ROW + (((4 * s + quad) ^ G::kswz(ql)) << 4));
+      st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, u), q[s], st, 0, 0, 0);
+    }
+    if (kb + 16 > lim0) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (kb + 4 * quad + k >= lim) st[k] = -INFINITY;
+      // keys that some pairs see and others do not
+      if (min(kb + 16, k1) > lim0) unsound = unsound || any_unsound<D>(V, 16);
+    }
+    const float bm = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3])) * c2;
+    if (__any(bm > m + kRescale)) {
+      const float mn = fmaxf(m, quad_max(bm));
+      const float sc = __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= sc;
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e) o[e] *= sc;
+    }
+    bf16x4_t pb;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(st[k], c2, -m));
+      l += p;
+      pb[k] = (__bf16)p;
+    }
+    // V^T: 16 lanes read four keys x 16 columns, lane i receives column i of the four keys
+    const int vr = (lane >> 2) & 3, vrow = 4 * quad + vr;
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) {
+      const bf16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+          (ltr_t)(V + vrow * G::ROW + (((2 * e) ^ G::vswz(vr)) << 4) + (lane & 3) * 8));
+      o[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, v), __builtin_bit_cast(s16x4_t, pb),
+                                                       o[e], 0, 0, 0);
+    }
   }
-  w.l = half_sum(w.l);
+  l = quad_sum(l);
+  if (unsound) {
+    KeyByKey<D, 16> kk;
+    kk.start();
+    for (int i = 0; i < blocks; ++i) {
+      const int kb = k0 + 16 * (wave + kWaves * i);
+      kk.add(a, ld, t.table, q, kb, min(kb + 16, k1), lim);
+    }
+    m = kk.m;
+    l = kk.l;
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) o[e] = kk.o[e];
+  }
 
   // the waves' results, joined: part [wave][pair][PART_ROW], then [m, l][wave][pair]
   __syncthreads();
   float* part = reinterpret_cast<float*>(smem);
-  float* ml = part + kWaves * 32 * SH::PART_ROW;
-  const int half = lane >> 5;
+  float* ml = part + kWaves * kThin * SH::PART_ROW;
 #pragma unroll
-  for (int e = 0; e < D / 32; ++e)
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *reinterpret_cast<float4*>(part + (wave * 32 + ql) * SH::PART_ROW + 32 * e + 8 * g + 4 * half) =
-          make_float4(w.o[e][4 * g], w.o[e][4 * g + 1], w.o[e][4 * g + 2], w.o[e][4 * g + 3]);
-  if (half == 0) {
-    ml[wave * 32 + ql] = w.m;
-    ml[(kWaves + wave) * 32 + ql] = w.l;
+  for (int e = 0; e < D / 16; ++e)
+    *reinterpret_cast<f32x4_t*>(part + (wave * kThin + ql) * SH::PART_ROW + 16 * e + 4 * quad) = o[e];
+  if (quad == 0) {
+    ml[wave * kThin + ql] = m;
+    ml[(kWaves + wave) * kThin + ql] = l;
   }
   __syncthreads();
-  constexpr int E = D / 8;                            // elements of a thread, eight threads to a pair
-  const int c = tid >> 3, e0 = (tid & 7) * E;
-  const Out u = place_of(a, t, prefix, h, t.x0 + c, chunk_keys, chunk, pp);
-  if (u.row < 0) return;
+  constexpr int E = D / 16;                           // elements of a thread, sixteen threads to a pair
+  const int c = tid >> 4, e0 = (tid & 15) * E, xc = t.x0 + c;
+  if (xc >= t.pairs) return;
+  const Out u = prefix ? prefix_place(a, t, h, xc, chunk)
+                       : own_place(a, t, h, xc, chunk, ceil_div(sees(a, t, false, xc / r), chunk_keys), pre);
+  if (u.pair < 0) return;
   float M = kLowest, L = 0.0f, acc[E];
 #pragma unroll
-  for (int v = 0; v < kWaves; ++v) M = fmaxf(M, ml[v * 32 + c]);
+  for (int v = 0; v < kWaves; ++v) M = fmaxf(M, ml[v * kThin + c]);
 #pragma unroll
   for (int e = 0; e < E; ++e) acc[e] = 0.0f;
 #pragma unroll
   for (int v = 0; v < kWaves; ++v) {
-    const float f = __builtin_amdgcn_exp2f(ml[v * 32 + c] - M);
-    L = fmaf(ml[(kWaves + v) * 32 + c], f, L);
+    const float f = __builtin_amdgcn_exp2f(ml[v * kThin + c] - M);
+    L = fmaf(ml[(kWaves + v) * kThin + c], f, L);
 #pragma unroll
-    for (int e = 0; e < E; e += 4) {
-      const float4 x = *reinterpret_cast<const float4*>(part + (v * 32 + c) * SH::PART_ROW + e0 + e);
-      acc[e] = fmaf(x.x, f, acc[e]);
-      acc[e + 1] = fmaf(x.y, f, acc[e + 1]);
-      acc[e + 2] = fmaf(x.z, f, acc[e + 2]);
-      acc[e + 3] = fmaf(x.w, f, acc[e + 3]);
-    }
+    for (int e = 0; e < E; ++e) acc[e] = fmaf(part[(v * kThin + c) * SH::PART_ROW + e0 + e], f, acc[e]);
   }
-  if ((tid & 7) == 0) store_ml(a, u, M, L);
-  const int64_t pair = u.row * a.shape.q_heads + u.head;
+  if ((tid & 15) == 0) store_ml(a, u, M, L);
   if (u.done) {
     const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-    __bf16* dst = static_cast<__bf16*>(a.O) + pair * D + e0;
+    __bf16* dst = static_cast<__bf16*>(a.O) + u.pair * D + e0;
 #pragma unroll
-    for (int e = 0; e < E; e += 8) {
-      bf16x8_t v;
+    for (int e = 0; e < E; e += 4) {
+      bf16x4_t v;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = (__bf16)(acc[e + k] * inv);
-      *reinterpret_cast<bf16x8_t*>(dst + e) = v;
+      for (int k = 0; k < 4; ++k) v[k] = (__bf16)(acc[e + k] * inv);
+      *reinterpret_cast<bf16x4_t*>(dst + e) = v;
     }
   } else {
-    float* dst = a.part_o + (pair * u.parts + u.part) * D + e0;
 #pragma unroll
     for (int e = 0; e < E; e += 4)
-      *reinterpret_cast<float4*>(dst + e) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+      *reinterpret_cast<float4*>(u.o + e0 + e) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
   }
 }
 
 // ---------------------------------------------------------------- the tall tiles
 
-// 128 pairs, 32 a wave; the waves share tiles of 64 keys, two deep.
+// One wave's 32 pairs: lane l holds pair l % 32; of 32 keys' scores those of keys
+// 8 (i / 4) + 4 (l / 32) + i % 4 in register i, and of the output elements
+// 32 t + 8 (i / 4) + 4 (l / 32) + i % 4 in o[t][i] (v_mfma_f32_32x32x16_bf16 with
+// keys, then values, as the row operand: S^T = K Q^T, O^T += V^T P).
 template <int D>
-__global__ __launch_bounds__(64 * kWaves, 2) void tall_kernel(AttendArgs a, int prefix) {
+struct Pairs {
+  bf16x8_t q[D / 16];
+  f32x16_t o[D / 32];
+  float m, l;             // m is the pair's, l this lane's share
+};
+
+// Scores of 64 keys in the LDS tile K.
+template <int D>
+__device__ __forceinline__ void scores(const Pairs<D>& w, const char* K, f32x16_t (&st)[2]) {
   using G = Geo<D>;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * 4 * G::BLOCK];     // [buffer][K, V][64 keys]
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, half = lane >> 5;
-  const int h = blockIdx.y, chunk = blockIdx.z;
-  if (blockIdx.x == 0 && h == 0 && chunk == 0 && prefix) report_entries(a, prefix);
-  Tile t;
-  if (!find_tile<kTall>(a, prefix, blockIdx.x, t)) return;
-  if (!prefix && t.pairs <= kThin) return;                                   // a thin tile's
-  const int chunk_keys = prefix ? a.plan.chunk_prefix : a.plan.chunk_tall;
-  const int pp = prefix ? 0 : prefix_parts(a, t.seg);
-  const int r = ratio(a);
-  const int tile_end = sees(a, t, prefix, (min(t.x0 + kTall, t.pairs) - 1) / r);
-  const int k0 = chunk * chunk_keys;
-  if (k0 >= tile_end && (prefix || chunk > 0)) return;
-  const int k1 = min(tile_end, k0 + chunk_keys);
+  const int lane = threadIdx.x & 63, ql = lane & 31, half = lane >> 5;
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) st[n][i] = 0.0f;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const uint4 u = *reinterpret_cast<const uint4*>(K + (32 * n + ql) * G::ROW +
+                                                      (((2 * s + half) ^ G::kswz(ql)) << 4));
+      st[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, u), w.q[s], st[n], 0, 0, 0);
+    }
+}
+
+// Hides keys from `lim` on (counted in the tile).
+__device__ __forceinline__ void hide(f32x16_t (&st)[2], int lim) {
+  const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (32 * n + 8 * (i >> 2) + 4 * half + (i & 3) >= lim) st[n][i] = -INFINITY;
+}
+
+// The running maximum moves, and the sums are rescaled, only when a score exceeds it
+// by more than 2^8, which float32 sums hold with the same relative error.
+template <int D>
+__device__ __forceinline__ void move_max(Pairs<D>& w, const f32x16_t (&st)[2], float c2) {
+  float bm = st[0][0];
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) bm = fmaxf(bm, st[n][i]);
+  bm *= c2;
+  if (__any(bm > w.m + kRescale)) {
+    const float mn = fmaxf(w.m, half_max(bm));
+    const float sc = __builtin_amdgcn_exp2f(w.m - mn);
+    w.m = mn;
+    w.l *= sc;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w.o[t][i] *= sc;
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void weights(Pairs<D>& w, const f32x16_t (&st)[2], bf16x8_t (&pb)[4], float c2) {
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(st[n][i], c2, -w.m));
+      w.l += p;
+      pb[2 * n + (i >> 3)][i & 7] = (__bf16)p;
+    }
+}
+
+// The probabilities a lane holds are its half of the operand's k slots as they stand:
+// slot 8 (l / 32) + j is key 4 (l / 32) + j for j < 4 and 8 + 4 (l / 32) + j - 4 for
+// j >= 4.  The value operand is read from the row-major tile by the transposing LDS
+// read: 16 lanes read four keys x 16 columns, lane i receives column i of the four.
+template <int D>
+__device__ __forceinline__ void add_values(Pairs<D>& w, const char* V, const bf16x8_t (&pb)[4]) {
+  using G = Geo<D>;
+  const int lane = threadIdx.x & 63, vr = (lane >> 2) & 3;
+  const char* base = V + (4 * (lane >> 5) + vr) * G::ROW + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+#pragma unroll
+  for (int g = 0; g < 4; ++g)
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) {
+      const int piece = (4 * t ^ G::vswz(vr)) << 4;
+      const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((ltr_t)(base + piece + 16 * g * G::ROW));
+      const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((ltr_t)(base + piece + (16 * g + 8) * G::ROW));
+      const bf16x8_t v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      w.o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pb[g], w.o[t], 0, 0, 0);
+    }
+}
+
+// 128 pairs, 32 a wave; the waves share tiles of 64 keys, K and V two deep each.  While
+// the vector units weigh one tile's scores, the next tile's are on the matrix cores.
+// Keys: a fused tile takes its prefix's steps first (the last one may be ragged), then
+// its own run's.
+template <int D>
+__device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool prefix, const Tile& t, int h, int chunk) {
+  using G = Geo<D>;
+  constexpr int STEP = kTallStep * G::ROW;                                    // 64 keys of K or V
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int ql = lane & 31, half = lane >> 5, r = ratio(a);
+  int g, pre = 0, P = 0;                             // parts of the prefix apart; its tokens taken here
+  if (!prefix) {
+    P = prefix_of(a, t.seg, g);
+    if (t.pairs <= kFuse) {
+      pre = ceil_div(P, a.plan.chunk_prefix);
+      P = 0;
+    }
+  }
+  const int before = ceil_div(P, kTallStep);
+  const int chunk_steps = (prefix ? a.plan.chunk_prefix : a.plan.chunk_tall) / kTallStep;
+  const int end = sees(a, t, prefix, (min(t.x0 + kTall, t.pairs) - 1) / r);   // of the run, for the whole tile
+  const int v0 = chunk * chunk_steps;
+  const int n = min(before + ceil_div(end, kTallStep) - v0, chunk_steps);     // steps of this chunk
+  if (n <= 0 && (prefix || chunk > 0)) return;
 
   const int xw = t.x0 + 32 * wave, x = xw + ql;
+  const bool idle = xw >= t.pairs;                                            // the wave has no pair
+  const bool live = x < t.pairs;
+  const int row = live ? x / r : 0;
   Pairs<D> w;
-  init_pairs(w);
-  load_queries<D>(a, t, prefix, h, x, xw, w);
-  // keys that this wave needs: none without a pair
-  const int wave_end = xw >= t.pairs ? 0 : min(k1, sees(a, t, prefix, (min(xw + 32, t.pairs) - 1) / r));
-
-  const int page_mask = (1 << a.shape.page_shift) - 1;
-  const Pages pages{t.table, a.shape.page_shift - 4, a.shape.pages, (t.len + 15) >> 4};
-  const char* Kc = static_cast<const char*>(a.k_cache);
-  const char* Vc = static_cast<const char*>(a.v_cache);
-  const int tiles = k1 > k0 ? (k1 - k0 + kTallStep - 1) / kTallStep : 0;
-  int pg = 0;                                        // lane l: the page of block 64 (i / 16) + l of the chunk
-  auto issue = [&](int i) {
-    if ((i & 15) == 0) pg = pages.load((k0 >> 4) + 4 * i, a.err);
-    const int kb = k0 + kTallStep * i;
-    char* K = smem + (i & 1) * 4 * G::BLOCK;
+  const uint16_t* qsrc =
+      static_cast<const uint16_t*>(a.Q) + (t.row0 + row) * a.ldq + (h * r + (x - row * r)) * D + 8 * half;
 #pragma unroll
-    for (int j = 0; j < 2 * G::LOADS / kWaves; ++j) {
-      const int row0 = (wave + kWaves * j) * G::LOAD_ROWS;
-      const int64_t head_page =
-          (int64_t)__builtin_amdgcn_readlane(pg, 4 * (i & 15) + (row0 >> 4)) * a.shape.kv_heads + h;
-      load_group<D>(Kc, Vc, head_page, page_mask, kb + row0, row0, k1, K, K + 2 * G::BLOCK);
-    }
-  };
-  if (tiles > 0) issue(0);
-  for (int i = 0; i < tiles; ++i) {
-    wait_vmcnt<0>();                                 // this wave's loads of tile i
-    __syncthreads();                                 // every wave's; and all are past tile i - 1
-    if (i + 1 < tiles) issue(i + 1);
-    const int kb = k0 + kTallStep * i;
-    const char* K = smem + (i & 1) * 4 * G::BLOCK;
-    if (kb < wave_end) step<D, 2>(w, K, K + 2 * G::BLOCK, kb, k1, a.c2, [] {});
+  for (int s = 0; s < D / 16; ++s) {
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (live) u = *reinterpret_cast<const uint4*>(qsrc + 16 * s);
+    w.q[s] = __builtin_bit_cast(bf16x8_t, u);
   }
-  w.l = half_sum(w.l);
-
-  const Out u = place_of(a, t, prefix, h, x, chunk_keys, chunk, pp);
-  if (u.row < 0) return;
-  if (half == 0) store_ml(a, u, w.m, w.l);
-  const int64_t pair = u.row * a.shape.q_heads + u.head;
-  const float inv = w.l == 0.0f ? 0.0f : 1.0f / w.l;
-  __bf16* out = static_cast<__bf16*>(a.O) + pair * D;
-  float* dst = a.part_o + (pair * u.parts + u.part) * D;
 #pragma unroll
   for (int e = 0; e < D / 32; ++e)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int c = 32 * e + 8 * g + 4 * half;
-      if (u.done) {
+    for (int i = 0; i < 16; ++i) w.o[e][i] = 0.0f;
+  w.m = kLowest;
+  w.l = 0.0f;
+  const int lim = live ? sees(a, t, prefix, row) : 0, lim0 = idle ? 0 : sees(a, t, prefix, xw / r);
+  const float c2 = a.c2;
+
+  // the wave loads keys 16 wave .. of every step: one page
+  Loader<D> ld;
+  ld.init(a, h);
+  int32_t* const err = a.err;
+  Window kw, vw, own;
+  if (v0 < before) {
+    kw.start(a, a.prefix.table + (int64_t)g * a.prefix.width, P, v0 * kTallStep);
+    own.start(a, t.table, t.len, 0);
+  } else {
+    kw.start(a, t.table, t.len, (v0 - before) * kTallStep);
+    own = kw;
+  }
+  vw = kw;
+  auto issue = [&](auto values, Window& win, int i) {
+    constexpr bool VALUES = decltype(values)::value;
+    const int v = v0 + i;
+    if (v == before && i > 0) win = own;
+    const int key0 = (v < before ? v : v - before) * kTallStep + 16 * wave;
+    ld.template load<VALUES>(win.page(key0 >> ld.shift, err), key0, v < before ? P : end,
+                             smem + ((VALUES ? 2 : 0) + (i & 1)) * STEP + 16 * wave * G::ROW);
+  };
+  // keys of step i that the lane's pair sees, counted in the step; the wave's first pair; all
+  auto seen = [&](int i, int of_run) { return v0 + i < before ? P - (v0 + i) * kTallStep
+                                                              : of_run - (v0 + i - before) * kTallStep; };
+  bool unsound = false;
+  if (n > 0) {
+    issue(std::false_type{}, kw, 0);
+    issue(std::true_type{}, vw, 0);
+    if (n > 1) issue(std::false_type{}, kw, 1);
+    f32x16_t st[2];
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (!idle) {
+      scores(w, smem, st);
+      if (seen(0, lim0) < kTallStep) hide(st, seen(0, lim));
+      move_max(w, st, c2);
+    }
+    for (int i = 0; i < n; ++i) {
+      wait_vmcnt<0>();                               // this wave's loads of K i + 1 and V i
+      __syncthreads();                               // every wave's; and all are past K i and V i - 1
+      if (i + 2 < n) issue(std::false_type{}, kw, i + 2);
+      if (i + 1 < n) issue(std::true_type{}, vw, i + 1);
+      if (idle) continue;
+      const char* V = smem + (2 + (i & 1)) * STEP;
+      // keys that some pairs of the wave see and others do not
+      if (min(seen(i, end), kTallStep) > max(seen(i, lim0), 0)) unsound = unsound || any_unsound<D>(V, kTallStep);
+      bf16x8_t pb[4];
+      f32x16_t nx[2];
+      if (i + 1 < n) scores(w, smem + ((i + 1) & 1) * STEP, nx);
+      weights(w, st, pb, c2);
+      add_values(w, V, pb);
+      if (i + 1 < n) {
+        if (seen(i + 1, lim0) < kTallStep) hide(nx, seen(i + 1, lim));
+        move_max(w, nx, c2);
+      }
+      st[0] = nx[0];
+      st[1] = nx[1];
+    }
+  }
+  w.l = half_sum(w.l);
+  if (unsound) {
+    KeyByKey<D, 32> kk;
+    kk.start();
+    for (int i = 0; i < n; ++i) {
+      const bool p = v0 + i < before;
+      const int kb = (p ? v0 + i : v0 + i - before) * kTallStep;
+      kk.add(a, ld, p ? a.prefix.table + (int64_t)g * a.prefix.width : t.table, w.q, kb,
+             min(kb + kTallStep, p ? P : end), p ? P : lim);
+    }
+    w.m = kk.m;
+    w.l = kk.l;
+#pragma unroll
+    for (int e = 0; e < D / 8; ++e)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w.o[e >> 2][4 * (e & 3) + k] = kk.o[e][k];
+  }
+
+  if (!live) return;
+  const int row_steps = before + ceil_div(lim, kTallStep);
+  const Out u = prefix ? prefix_place(a, t, h, x, chunk) : own_place(a, t, h, x, chunk, ceil_div(row_steps, chunk_steps), pre);
+  if (u.pair < 0) return;
+  if (half == 0) store_ml(a, u, w.m, w.l);
+  if (u.done) {
+    const float inv = w.l == 0.0f ? 0.0f : 1.0f / w.l;
+    __bf16* dst = static_cast<__bf16*>(a.O) + u.pair * D + 4 * half;
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4) {
         bf16x4_t v;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = (__bf16)(w.o[e][4 * g + k] * inv);
-        *reinterpret_cast<bf16x4_t*>(out + c) = v;
-      } else {
-        *reinterpret_cast<float4*>(dst + c) =
-            make_float4(w.o[e][4 * g], w.o[e][4 * g + 1], w.o[e][4 * g + 2], w.o[e][4 * g + 3]);
+        for (int k = 0; k < 4; ++k) v[k] = (__bf16)(w.o[e][4 * g4 + k] * inv);
+        *reinterpret_cast<bf16x4_t*>(dst + 32 * e + 8 * g4) = v;
       }
-    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4)
+        *reinterpret_cast<float4*>(u.o + 32 * e + 8 * g4 + 4 * half) =
+            make_float4(w.o[e][4 * g4], w.o[e][4 * g4 + 1], w.o[e][4 * g4 + 2], w.o[e][4 * g4 + 3]);
+  }
+}
+
+// One launch for all tiles: the prefixes' (thin or tall), the sequences' tall ones, the
+// sequences' thin ones, in this order.
+template <int D>
+__global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a) {
+  __shared__ __attribute__((aligned(1024))) char smem[kAttendLds];
+  const AttendPlan& p = a.plan;
+  const int heads = a.shape.kv_heads;
+  int id = blockIdx.x;
+  if (id == 0) {
+    report_entries(a, false);
+    if (a.prefix.count > 0) report_entries(a, true);
+  }
+  Tile t;
+  // block id of `tiles` tiles, the key heads and the chunks
+  const int tall = p.prefix_tall && id < p.prefix_blocks ? 1 : id >= p.prefix_blocks && id < p.prefix_blocks + p.tall_blocks ? 2 : 0;
+  if (tall) {
+    const bool prefix = tall == 1;
+    if (!prefix) id -= p.prefix_blocks;
+    const int tiles = prefix ? p.prefix_tiles : p.tall_tiles;
+    const int rest = id / tiles, tile = tiles - 1 - (id - rest * tiles);
+    if (!find_tile<kTall>(a, prefix, tile, t)) return;
+    if (!prefix && t.pairs <= kThin) return;                                 // a thin tile's
+    tall_tile<D>(a, smem, prefix, t, rest % heads, rest / heads);
+    return;
+  }
+  const bool prefix = id < p.prefix_blocks;
+  if (!prefix) id -= p.prefix_blocks + p.tall_blocks;
+  const int tiles = prefix ? p.prefix_tiles : a.runs.count;
+  const int rest = id / tiles, tile = id - rest * tiles;
+  if (prefix) {
+    if (!find_tile<kThin>(a, true, tile, t)) return;
+  } else {                                           // a sequence to a tile; longer ones are the tall tiles'
+    t.seg = tile;
+    if (rows_of(a.rows, t.seg, t.row0, t.n) != SP_DEV_OK) return;
+    const int64_t pairs = (int64_t)t.n * ratio(a);
+    if (pairs == 0 || pairs > kThin || tokens_of(a.runs, t.seg, t.len) != SP_DEV_OK) return;
+    t.pairs = (int)pairs;
+    t.x0 = 0;
+    t.table = a.runs.table + (int64_t)t.seg * a.runs.width;
+  }
+  thin_tile<D>(a, smem, prefix, t, rest % heads, rest / heads);
 }
 
 // ---------------------------------------------------------------- float32
@@ -647,18 +882,26 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tall_kernel(AttendArgs a, int 
 //   scores of keys 4 (l / 16) + i of pair l % 16;
 //   O^T += V^T P: lane l holds element l % 16 of each 16 of the keys 4 (l / 16) + i.
 template <int D>
-__global__ __launch_bounds__(64 * kWaves) void attend_f32_kernel(AttendArgs a, int prefix) {
+__global__ __launch_bounds__(64 * kWaves) void attend_f32_kernel(AttendArgs a) {
   constexpr int PART_ROW = D + 4;
-  __shared__ __attribute__((aligned(16))) float smem[kWaves * 16 * (PART_ROW + 2)];
+  __shared__ __attribute__((aligned(16))) float smem[kWaves * kThin * (PART_ROW + 2)];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 15, quad = lane >> 4;
-  const int h = blockIdx.y, chunk = blockIdx.z;
-  if (blockIdx.x == 0 && h == 0 && chunk == 0) report_entries(a, prefix);
+  int id = blockIdx.x;
+  if (id == 0) {
+    report_entries(a, false);
+    if (a.prefix.count > 0) report_entries(a, true);
+  }
+  const bool prefix = id < a.plan.prefix_blocks;
+  if (!prefix) id -= a.plan.prefix_blocks;
+  const int tiles = prefix ? a.plan.prefix_tiles : a.plan.thin_tiles;
+  const int rest = id / tiles, h = rest % a.shape.kv_heads, chunk = rest / a.shape.kv_heads;
   Tile t;
-  if (!find_tile<kThinF32>(a, prefix, blockIdx.x, t)) return;
+  if (!find_tile<kThin>(a, prefix, id - rest * tiles, t)) return;
   const int chunk_keys = prefix ? a.plan.chunk_prefix : a.plan.chunk_thin;
-  const int pp = prefix ? 0 : prefix_parts(a, t.seg);
+  int gi;
+  const int pre = prefix ? 0 : ceil_div(prefix_of(a, t.seg, gi), a.plan.chunk_prefix);
   const int r = ratio(a);
-  const int tile_end = sees(a, t, prefix, (min(t.x0 + kThinF32, t.pairs) - 1) / r);
+  const int tile_end = sees(a, t, prefix, (min(t.x0 + kThin, t.pairs) - 1) / r);
   const int k0 = chunk * chunk_keys;
   if (k0 >= tile_end && (prefix || chunk > 0)) return;
   const int k1 = min(tile_end, k0 + chunk_keys);
@@ -681,14 +924,12 @@ __global__ __launch_bounds__(64 * kWaves) void attend_f32_kernel(AttendArgs a, i
   for (int e = 0; e < D / 16; ++e) o[e] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   float m = kLowest, l = 0.0f;
   const int page_mask = (1 << a.shape.page_shift) - 1;
-  const Pages pages{t.table, a.shape.page_shift - 4, a.shape.pages, (t.len + 15) >> 4};
   const int blocks = k1 - k0 > 16 * wave ? (k1 - k0 - 16 * wave + 16 * kWaves - 1) / (16 * kWaves) : 0;
-  int pg = 0;                                        // lane l: the page of block i - i % 16 + l / 4 of wave l % 4
+  Window win;
+  if (blocks > 0) win.start(a, t.table, t.len, k0 + 16 * wave);
   for (int i = 0; i < blocks; ++i) {
-    if ((i & 15) == 0) pg = pages.load((k0 >> 4) + 4 * i, a.err);
     const int kb = k0 + 16 * (wave + kWaves * i);
-    const int64_t head_page =
-        (int64_t)__builtin_amdgcn_readlane(pg, 4 * (i & 15) + wave) * a.shape.kv_heads + h;
+    const int64_t head_page = (int64_t)win.page(kb >> a.shape.page_shift, a.err) * a.shape.kv_heads + h;
     const int64_t at = (head_page * (page_mask + 1) + (kb & page_mask)) * D;
     const float* K = static_cast<const float*>(a.k_cache) + at;
     const float* V = static_cast<const float*>(a.v_cache) + at;
@@ -732,7 +973,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_f32_kernel(AttendArgs a, i
       st[g] = exp2f(fmaf(st[g], a.c2, -m));
       l += st[g];
     }
-    if (masked && min(kb + 16, k1) > lim0) {         // as in the bfloat16 step
+    if (masked && min(kb + 16, k1) > lim0) {         // a hidden key's value would be weighed with 0
       bool bad = false;
 #pragma unroll
       for (int e = 0; e < D / 16; ++e)
@@ -775,8 +1016,11 @@ __global__ __launch_bounds__(64 * kWaves) void attend_f32_kernel(AttendArgs a, i
   __syncthreads();
   constexpr int E = D / 16;                          // sixteen threads to a pair
   const int c = tid >> 4, e0 = (tid & 15) * E;
-  const Out u = place_of(a, t, prefix, h, t.x0 + c, chunk_keys, chunk, pp);
-  if (u.row < 0) return;
+  const int xc = t.x0 + c;
+  if (xc >= t.pairs) return;
+  const Out u = prefix ? prefix_place(a, t, h, xc, chunk)
+                       : own_place(a, t, h, xc, chunk, ceil_div(sees(a, t, false, xc / r), chunk_keys), pre);
+  if (u.pair < 0) return;
   float M = kLowest, L = 0.0f, acc[E];
 #pragma unroll
   for (int y = 0; y < kWaves; ++y) M = fmaxf(M, ml[y * 16 + c]);
@@ -790,9 +1034,8 @@ __global__ __launch_bounds__(64 * kWaves) void attend_f32_kernel(AttendArgs a, i
     for (int e = 0; e < E; ++e) acc[e] = fmaf(smem[(y * 16 + c) * PART_ROW + e0 + e], f, acc[e]);
   }
   if ((tid & 15) == 0) store_ml(a, u, M, L);
-  const int64_t pair = u.row * a.shape.q_heads + u.head;
   const float inv = !u.done ? 1.0f : L == 0.0f ? 0.0f : 1.0f / L;
-  float* dst = u.done ? static_cast<float*>(a.O) + pair * D : a.part_o + (pair * u.parts + u.part) * D;
+  float* dst = u.done ? static_cast<float*>(a.O) + u.pair * D : u.o;
 #pragma unroll
   for (int e = 0; e < E; e += 4)
     *reinterpret_cast<float4*>(dst + e0 + e) =
@@ -801,133 +1044,204 @@ __global__ __launch_bounds__(64 * kWaves) void attend_f32_kernel(AttendArgs a, i
 
 // ---------------------------------------------------------------- joining the parts
 
-// One wave to a (row, head): the parts' maxima and sums, then their outputs.
-template <typename T, int D>
-__global__ __launch_bounds__(64 * kWaves) void combine_kernel(AttendArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t pair = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-  const int64_t row = pair / a.shape.q_heads;
-  if (row >= a.rows.rows) return;
-  // rows of no sequence have no count of parts
-  if (a.rows.padded) {
-    const int64_t s = a.rows.rows_per_seq > 0 ? row / a.rows.rows_per_seq : a.runs.count;
-    if (s >= a.runs.count || row - s * a.rows.rows_per_seq >= a.rows.info[s]) return;
-  } else if (row < a.rows.info[0] || row >= a.rows.info[a.runs.count]) {
-    return;
+// SPLIT waves to a (row, head): each joins every SPLIT-th part, and they join through LDS.
+// Pairs of the short sequences, or (tall) of the rows of the others.
+template <typename T, int D, int SPLIT>
+__global__ __launch_bounds__(64 * kWaves) void combine_kernel(AttendArgs a, int tall) {
+  constexpr int E = D / 64, AHEAD = 8;
+  __shared__ float red[kWaves][D + 2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, share = wave % SPLIT;
+  const int64_t at = (int64_t)blockIdx.x * (kWaves / SPLIT) + wave / SPLIT;
+  const int Hq = a.shape.q_heads;
+  const AttendPlan& p = a.plan;
+  int64_t row = -1, base = 0;                        // the row's parts from pair `base` on
+  const int head = (int)(at % Hq);
+  if (tall) {
+    row = at / Hq;
+    base = row * Hq;
+    bool live = row < a.rows.rows;
+    if (live && a.rows.padded) {
+      const int64_t s = row / a.rows.rows_per_seq;
+      live = s < a.runs.count && row - s * a.rows.rows_per_seq < a.rows.info[s] &&
+             a.rows.info[s] * (int64_t)ratio(a) > p.short_pairs;
+    } else if (live) {
+      const int s = wave_find_last(a.runs.count, row, [&](int i) { return (int64_t)a.rows.info[i]; });
+      live = row >= a.rows.info[s] && row < a.rows.info[s + 1] &&
+             (a.rows.info[s + 1] - a.rows.info[s]) * (int64_t)ratio(a) > p.short_pairs;
+    }
+    if (!live) row = -1;
+  } else {
+    const int64_t per = (int64_t)p.short_rows * Hq, s = at / per;
+    int64_t first;
+    int n;
+    if (s < a.runs.count && rows_of(a.rows, (int)s, first, n) == SP_DEV_OK) {
+      const int i = (int)((at - s * per) / Hq);
+      if (i < n && (int64_t)n * ratio(a) <= p.short_pairs) {
+        row = first + i;
+        base = short_base(a, (int)s, i);
+      }
+    }
   }
-  const int code = a.row_parts[row], own = code & 0xffff, pre = code >> 16;
-  if (code == 0 || own > a.plan.own_parts || pre > a.plan.prefix_parts) return;
-  const int parts = a.plan.prefix_parts + a.plan.own_parts;
-  const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + pair * parts;
-  const float* po = a.part_o + pair * parts * D;
-  auto slot = [&](int i) { return i < pre ? i : a.plan.prefix_parts + i - pre; };
-  float M = kLowest;
-  for (int i = lane; i < pre + own; i += 64) M = fmaxf(M, ml[slot(i)].x);
-  for (int s = 32; s >= 1; s >>= 1) M = fmaxf(M, __shfl_xor(M, s, 64));
-  constexpr int E = D / 64;
-  float L = 0.0f, acc[E] = {};
-  for (int i = 0; i < pre + own; ++i) {
-    const int p = slot(i);
-    const float f = exp2f(ml[p].x - M);
-    L = fmaf(ml[p].y, f, L);
+  int own = 0, pre = 0;
+  if (row >= 0) {
+    const int2 c = a.row_parts[row];
+    own = c.x;
+    pre = c.y;
+    // (after an error in the batch's entries a row may have no count)
+    if (own < 0 || own > (tall ? p.tall_parts : p.short_parts) || pre < 0 || pre > p.prefix_parts) own = pre = 0;
+  }
+  const int total = own + pre;
+  if (SPLIT == 1 && total == 0) return;
+  const int64_t pair = base + head;
+  const float2* pml = reinterpret_cast<const float2*>(a.prefix_ml) + pair * p.prefix_parts;
+  const float* po = a.prefix_o + pair * p.prefix_parts * D;
+  const float2* oml = reinterpret_cast<const float2*>(tall ? a.tall_ml : a.short_ml) + pair * (tall ? p.tall_parts : p.short_parts);
+  const float* oo = (tall ? a.tall_o : a.short_o) + pair * (tall ? p.tall_parts : p.short_parts) * D;
+  float M = kLowest, L = 0.0f, acc[E] = {};
+  for (int i0 = share; i0 < total; i0 += SPLIT * AHEAD) {
+    float2 ml[AHEAD];
+    float v[AHEAD][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = fmaf(po[(int64_t)p * D + E * lane + e], f, acc[e]);
+    for (int k = 0; k < AHEAD; ++k) {
+      const int i = i0 + SPLIT * k;
+      ml[k] = make_float2(kLowest, 0.0f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[k][e] = 0.0f;
+      if (i < total) {
+        ml[k] = i < pre ? pml[i] : oml[i - pre];
+        const float* src = i < pre ? po + (int64_t)i * D : oo + (int64_t)(i - pre) * D;
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[k][e] = src[E * lane + e];
+      }
+    }
+    float mn = M;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) mn = fmaxf(mn, ml[k].x);
+    const float f0 = exp2f(M - mn);
+    M = mn;
+    L *= f0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] *= f0;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const float f = exp2f(ml[k].x - M);
+      L = fmaf(ml[k].y, f, L);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = fmaf(v[k][e], f, acc[e]);
+    }
+  }
+  if constexpr (SPLIT > 1) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) red[wave][E * lane + e] = acc[e];
+    if (lane == 0) {
+      red[wave][D] = M;
+      red[wave][D + 1] = L;
+    }
+    __syncthreads();
+    if (share != 0 || total == 0) return;
+#pragma unroll
+    for (int k = 1; k < SPLIT; ++k) {
+      const float mk = red[wave + k][D], mn = fmaxf(M, mk);
+      const float f = exp2f(M - mn), fk = exp2f(mk - mn);
+      M = mn;
+      L = fmaf(L, f, red[wave + k][D + 1] * fk);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = fmaf(acc[e], f, red[wave + k][E * lane + e] * fk);
+    }
   }
   const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+  const int64_t out = row * Hq + head;
 #pragma unroll
-  for (int e = 0; e < E; ++e) static_cast<T*>(a.O)[pair * D + E * lane + e] = (T)(acc[e] * inv);
-  if (a.lse && lane == 0) a.lse[pair] = lse_of(M, L);
+  for (int e = 0; e < E; ++e) static_cast<T*>(a.O)[out * D + E * lane + e] = (T)(acc[e] * inv);
+  if (a.lse && lane == 0) a.lse[out] = lse_of(M, L);
 }
 
-// Keys of a chunk: enough chunks that `tiles` tiles and key heads give the device
-// about `target` workgroups, of at least `least` keys each, in whole steps.
-inline int chunk_of(int64_t tiles, int max_len, int64_t target, int least, int step) {
-  int64_t parts = (target + tiles - 1) / tiles;
+// Keys of a chunk: enough chunks that `items` tiles and key heads give the device about
+// `target` workgroups, of at least `least` keys each, in whole steps.
+inline int chunk_of(int64_t items, int64_t max_len, int64_t target, int least, int step) {
+  int64_t parts = (target + items - 1) / items;
   const int64_t most = (max_len + least - 1) / least;
   if (parts > most) parts = most;
-  if (parts > 1024) parts = 1024;
+  if (parts > kMaxParts) parts = kMaxParts;
   if (parts < 1) parts = 1;
   const int64_t keys = (max_len + parts - 1) / parts;
   return (int)((keys + step - 1) / step * step) + (keys == 0 ? step : 0);
 }
 
-inline int parts_of(int max_len, int chunk) { return (max_len + chunk - 1) / chunk; }
+inline int parts_of(int64_t max_len, int chunk) { return (int)((max_len + chunk - 1) / chunk); }
 
 }  // namespace
 
 AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const CacheRuns& runs,
                              const CacheRuns& prefix) {
   AttendPlan p{};
-  const int64_t r = s.q_heads / s.kv_heads, pairs = rows.rows * r;
-  const int64_t S = runs.count > 0 ? runs.count : 1, G = prefix.count > 0 ? prefix.count : 1;
+  const int64_t r = s.q_heads / s.kv_heads, pairs = rows.rows * r, longest = rows.max_rows * r;
+  const int64_t heads = s.kv_heads, S = runs.count, G = prefix.count;
   const bool f32 = s.dtype == SP_F32;
-  p.prefix_tall = !f32 && prefix.count > 0 && pairs > (int64_t)kThin * G;
-  p.own_tall = !f32 && rows.max_rows * r > kThin;
-  const int thin = f32 ? kThinF32 : kThin, thin_step = f32 ? 16 * kWaves : kThinStep;
-  const int64_t heads = s.kv_heads;
-  p.chunk_thin = chunk_of((f32 ? pairs / thin + S : S) * heads, runs.max_len, 512, 256, thin_step);
-  p.chunk_tall = chunk_of((pairs / kTall + S) * heads, runs.max_len, 512, 512, kTallStep);
-  const int tile = p.prefix_tall ? kTall : thin;
-  p.chunk_prefix = chunk_of((pairs / tile + G) * heads, prefix.max_len, 512, p.prefix_tall ? 512 : 256,
-                            p.prefix_tall ? kTallStep : thin_step);
-  p.prefix_parts = prefix.count > 0 ? parts_of(prefix.max_len, p.chunk_prefix) : 0;
-  p.own_parts = parts_of(runs.max_len, p.chunk_thin);
-  if (p.own_tall && parts_of(runs.max_len, p.chunk_tall) > p.own_parts)
-    p.own_parts = parts_of(runs.max_len, p.chunk_tall);
+  const bool own_tall = !f32 && longest > kThin;
+  // float32 has no tall tiles: every sequence is short, and its prefix is shared
+  p.short_pairs = (int)(f32 || longest < kFuse ? longest : kFuse);
+  if (p.short_pairs < 1) p.short_pairs = 1;
+  p.short_rows = (int)((p.short_pairs + r - 1) / r);
+  p.thin_tiles = (int)(f32 ? pairs / kThin + S : S);
+  p.chunk_thin = chunk_of((p.thin_tiles > 0 ? p.thin_tiles : 1) * heads, runs.max_len, 2048, 256, kThinStep);
+  p.thin_blocks = p.thin_tiles * heads * (runs.max_len > 0 ? parts_of(runs.max_len, p.chunk_thin) : 1);
+  p.short_parts = parts_of(runs.max_len, p.chunk_thin);
+  if (own_tall) {
+    const int64_t keys = (prefix.max_len + kTallStep - 1) / kTallStep * kTallStep + (int64_t)runs.max_len;
+    p.tall_tiles = (int)(pairs / kTall + S);
+    p.chunk_tall = chunk_of((p.tall_tiles > 0 ? p.tall_tiles : 1) * heads, keys, 512, 512, kTallStep);
+    p.tall_parts = parts_of(keys, p.chunk_tall);
+    p.tall_blocks = p.tall_tiles * heads * (p.tall_parts > 0 ? p.tall_parts : 1);
+    if (p.tall_parts > p.short_parts) p.short_parts = p.tall_parts;
+  }
+  if (G > 0 && prefix.max_len > 0) {
+    p.prefix_tall = !f32 && pairs > kThin * G;
+    p.prefix_tiles = (int)(pairs / (p.prefix_tall ? kTall : kThin) + G);
+    p.chunk_prefix = p.prefix_tall ? chunk_of(p.prefix_tiles * heads, prefix.max_len, 512, 512, kTallStep)
+                                   : chunk_of(p.prefix_tiles * heads, prefix.max_len, 2048, 256, kThinStep);
+    p.prefix_parts = parts_of(prefix.max_len, p.chunk_prefix);
+    p.prefix_blocks = p.prefix_tiles * heads * p.prefix_parts;
+  } else {
+    p.chunk_prefix = kTallStep;
+  }
   return p;
 }
 
 namespace {
 
-template <int D>
-void launch_tiles(const AttendArgs& a, hipStream_t stream) {
-  const AttendPlan& p = a.plan;
-  const int64_t r = a.shape.q_heads / a.shape.kv_heads, pairs = a.rows.rows * r;
-  const unsigned heads = (unsigned)a.shape.kv_heads, S = (unsigned)a.runs.count, G = (unsigned)a.prefix.count;
-  auto chunks = [](int max_len, int chunk) { return (unsigned)(max_len > 0 ? parts_of(max_len, chunk) : 1); };
+template <typename T, int D>
+void launch_combine(const AttendArgs& a, int64_t pairs, int parts, int tall, hipStream_t stream) {
   const dim3 block(64 * kWaves);
-  if (a.shape.dtype == SP_F32) {
-    if (p.prefix_parts > 0)
-      hipLaunchKernelGGL(attend_f32_kernel<D>, dim3((unsigned)(pairs / kThinF32) + G, heads, p.prefix_parts), block,
-                         0, stream, a, 1);
-    hipLaunchKernelGGL(attend_f32_kernel<D>,
-                       dim3((unsigned)(pairs / kThinF32) + S, heads, chunks(a.runs.max_len, p.chunk_thin)), block, 0,
-                       stream, a, 0);
-    return;
-  }
-  if (p.prefix_parts > 0) {
-    if (p.prefix_tall)
-      hipLaunchKernelGGL(tall_kernel<D>, dim3((unsigned)(pairs / kTall) + G, heads, p.prefix_parts), block, 0, stream,
-                         a, 1);
-    else
-      hipLaunchKernelGGL(thin_kernel<D>, dim3((unsigned)(pairs / kThin) + G, heads, p.prefix_parts), block, 0, stream,
-                         a, 1, 1);
-  }
-  if (p.own_tall)
-    hipLaunchKernelGGL(tall_kernel<D>,
-                       dim3((unsigned)(pairs / kTall) + S, heads, chunks(a.runs.max_len, p.chunk_tall)), block, 0,
-                       stream, a, 0);
-  hipLaunchKernelGGL(thin_kernel<D>, dim3(S, heads, chunks(a.runs.max_len, p.chunk_thin)), block, 0, stream, a, 0, 0);
+  if (parts > 16)
+    hipLaunchKernelGGL((combine_kernel<T, D, kWaves>), dim3((unsigned)pairs), block, 0, stream, a, tall);
+  else
+    hipLaunchKernelGGL((combine_kernel<T, D, 1>), dim3((unsigned)((pairs + kWaves - 1) / kWaves)), block, 0, stream, a,
+                       tall);
 }
 
-template <typename T>
-void launch_combine(const AttendArgs& a, hipStream_t stream) {
-  const int64_t pairs = a.rows.rows * a.shape.q_heads;
-  const dim3 grid((unsigned)((pairs + kWaves - 1) / kWaves)), block(64 * kWaves);
-  if (a.shape.head_dim == 128) hipLaunchKernelGGL((combine_kernel<T, 128>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((combine_kernel<T, 64>), grid, block, 0, stream, a);
+template <typename T, int D>
+void launch_attend(const AttendArgs& a, hipStream_t stream) {
+  const AttendPlan& p = a.plan;
+  const dim3 grid((unsigned)(p.prefix_blocks + p.tall_blocks + p.thin_blocks)), block(64 * kWaves);
+  if constexpr (std::is_same<T, float>::value)
+    hipLaunchKernelGGL(attend_f32_kernel<D>, grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL(attend_kernel<D>, grid, block, 0, stream, a);
+  if (p.prefix_parts > 0 || p.short_parts > 1)
+    launch_combine<T, D>(a, (int64_t)a.runs.count * p.short_rows * a.shape.q_heads, p.prefix_parts + p.short_parts, 0,
+                         stream);
+  if (p.tall_parts > 1 && a.rows.max_rows * (int64_t)(a.shape.q_heads / a.shape.kv_heads) > p.short_pairs)
+    launch_combine<T, D>(a, a.rows.rows * a.shape.q_heads, p.tall_parts, 1, stream);
 }
 
 }  // namespace
 
 hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t stream) {
   if (a.rows.rows == 0 || a.runs.count == 0) return hipSuccess;
-  if (a.shape.head_dim == 128) launch_tiles<128>(a, stream);
-  else launch_tiles<64>(a, stream);
-  if (a.plan.prefix_parts > 0 || a.plan.own_parts > 1) {
-    if (a.shape.dtype == SP_F32) launch_combine<float>(a, stream);
-    else launch_combine<__bf16>(a, stream);
-  }
+  const bool wide = a.shape.head_dim == 128;
+  if (a.shape.dtype == SP_F32) wide ? launch_attend<float, 128>(a, stream) : launch_attend<float, 64>(a, stream);
+  else wide ? launch_attend<__bf16, 128>(a, stream) : launch_attend<__bf16, 64>(a, stream);
   return hipGetLastError();
 }
 

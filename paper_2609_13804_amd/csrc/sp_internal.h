@@ -214,9 +214,12 @@ hipError_t launch_cache_append(AppendArgs a, hipStream_t stream);
 // times key heads in tiles, keys in chunks; a row's result over a chunk is a
 // part.
 struct AttendPlan {
-  int prefix_tall, own_tall;              // whether the tall tiles are launched
-  int chunk_prefix, chunk_thin, chunk_tall;
-  int prefix_parts, own_parts;            // most parts of a row
+  int chunk_prefix, chunk_thin, chunk_tall;         // keys of a chunk
+  int prefix_parts, short_parts, tall_parts;        // most parts of a row: over its prefix, its own keys
+  int short_pairs, short_rows;                      // the largest short sequence's pairs, rows
+  int prefix_tall;                                  // the prefixes' tiles are tall ones
+  int prefix_tiles, tall_tiles, thin_tiles;         // tiles of a key head
+  int64_t prefix_blocks, tall_blocks, thin_blocks;  // workgroups
 };
 struct AttendArgs {
   CacheShape shape;
@@ -234,9 +237,13 @@ struct AttendArgs {
   float* lse;
   AttendPlan plan;
   // workspace pieces
-  int32_t* row_parts;     // [rows]
-  float* part_ml;         // [rows, q_heads, parts, 2]
-  float* part_o;          // [rows, q_heads, parts, head_dim]
+  int2* row_parts;        // [rows]: parts over the row's own keys (0: it is done), over its prefix
+  float* short_ml;        // short sequences: [count, short_rows, q_heads, short_parts, 2]
+  float* short_o;         //                  [count, short_rows, q_heads, short_parts, head_dim]
+  float* prefix_ml;       // their prefixes:  [count, short_rows, q_heads, prefix_parts, 2]
+  float* prefix_o;        //                  [count, short_rows, q_heads, prefix_parts, head_dim]
+  float* tall_ml;         // the others:      [rows, q_heads, tall_parts, 2]
+  float* tall_o;          //                  [rows, q_heads, tall_parts, head_dim]
   int32_t* err;
 };
 AttendPlan plan_cache_attend(const CacheShape& shape, const CacheRows& rows, const CacheRuns& runs,

@@ -119,7 +119,8 @@ class Batch:
                                   nbytes, stream=stream)
         torch.cuda.synchronize()
         if check:
-            assert sp.stepprune_read_device_error(ws) == sp.SP_DEV_OK
+            code = sp.stepprune_read_device_error(ws)
+            assert code == sp.SP_DEV_OK, code
         self.ws = ws
         return o.double().cpu().numpy(), None if z is None else z.double().cpu().numpy()
 

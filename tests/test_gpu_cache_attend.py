@@ -121,10 +121,9 @@ def test_hidden_tokens_have_no_influence(gpu_lib, dtype, bad, D):
         b.upload()
     oc, lc = clean.attend()
     od, ld = dirty.attend()
-    tol, _ = clean.bounds(*clean.oracle())
-    # (a tile that holds such a value sums its keys one by one: another order, the same bound)
+    tol, tol_l = clean.bounds(*clean.oracle())
     assert (np.abs(od[:41] - oc[:41]) <= 2 * tol[:41]).all()
-    assert np.isfinite(od[:41]).all() and (ld[:41] == lc[:41]).all()
+    assert np.isfinite(od[:41]).all() and (np.abs(ld[:41] - lc[:41]) <= 2 * tol_l[:41]).all()
     assert not np.isfinite(od[41:, :2]).all()
 
 
