@@ -35,10 +35,13 @@ namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) bf16x4_t* ltr_t;
+typedef __attribute__((address_space(3))) char* lds_t;
 
 constexpr int kThin = 16, kTall = 128;     // pairs of a tile
 constexpr int kFuse = 64;                  // pairs of a sequence past which it takes its prefix by itself
@@ -51,8 +54,13 @@ constexpr int kTallStep = 64;
 constexpr float kLowest = -FLT_MAX;
 constexpr float kRescale = 8.0f;           // log2 of the largest unscaled probability
 
-// what lanes past the last key load
-__device__ __align__(16) const uint32_t zeros16[4] = {0, 0, 0, 0};
+// The kernel's arguments where they lie, read again from there: code after a long loop
+// that reads them through this keeps no scalar registers for them over the loop.
+__device__ __forceinline__ const AttendArgs& arguments() {
+  auto p = (const __attribute__((address_space(4))) AttendArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const AttendArgs*)p;
+}
 
 // ---------------------------------------------------------------- tiles
 
@@ -137,50 +145,52 @@ __device__ __forceinline__ int prefix_of(const AttendArgs& a, int s, int& g) {
   return len;
 }
 
+__device__ __forceinline__ const int32_t* pages_of(const AttendArgs& a, bool prefix, int i) {
+  return prefix ? a.prefix.table + (int64_t)i * a.prefix.width : a.runs.table + (int64_t)i * a.runs.width;
+}
+
 __device__ __forceinline__ int ceil_div(int x, int y) { return (x + y - 1) / y; }
 
-// A run's pages from page `base` on, 64 in a wave's lanes and the next 64 on their way.
-struct Window {
-  const int32_t* table;
-  int used, count;             // pages of the run, of the cache
-  int base, now, next;
-  __device__ __forceinline__ int fetch(int p0, int32_t* err) const {
-    const int i = p0 + (int)(threadIdx.x & 63);
-    int p = i < used ? table[i] : 0;
-    if ((uint32_t)p >= (uint32_t)count) {
-      set_device_error(err, SP_DEV_BAD_PAGE);
-      p = 0;
-    }
-    return p;
+__device__ __forceinline__ int checked_page(const AttendArgs& a, int page) {
+  if ((uint32_t)page < (uint32_t)a.shape.pages) return page;
+  set_device_error(a.err, SP_DEV_BAD_PAGE);
+  return 0;
+}
+
+// Where the keys from `key` on lie in the key array (the values: in the value array).
+template <int ROW>
+__device__ __forceinline__ int64_t place_of(const AttendArgs& a, int page, int h, int key) {
+  const int shift = a.shape.page_shift;
+  return (((int64_t)page * a.shape.kv_heads + h << shift) + (key & ((1 << shift) - 1))) * ROW;
+}
+
+// The lane's half of a 64-bit number that lane `from` holds, in scalar registers.
+__device__ __forceinline__ int64_t lane_value(uint32_t lo, uint32_t hi, int from) {
+  const uint32_t l = __builtin_amdgcn_readlane(lo, from), h = __builtin_amdgcn_readlane(hi, from);
+  return (int64_t)((uint64_t)h << 32 | l);
+}
+
+// Places of the 16-key blocks that a wave takes, one every STRIDE keys from `first` on:
+// lane j holds that of block 64 (i / 64) + j, and the page of the block 64 further on.
+template <int ROW, int STRIDE>
+struct Places {
+  uint32_t lo, hi;
+  int ahead;
+  __device__ __forceinline__ int fetch(const AttendArgs& a, const int32_t* table, int len, int first, int i) const {
+    const int key = first + STRIDE * (i + (int)(threadIdx.x & 63));
+    return checked_page(a, key < len ? table[key >> a.shape.page_shift] : 0);
   }
-  __device__ __forceinline__ void start(const AttendArgs& a, const int32_t* pages, int tokens, int key0) {
-    table = pages;
-    used = ceil_div(tokens, 1 << a.shape.page_shift);
-    count = a.shape.pages;
-    const int p0 = key0 >> a.shape.page_shift;
-    int32_t* const err = a.err;
-    base = p0;
-    now = fetch(p0, err);
-    next = fetch(p0 + 64, err);
-  }
-  // page i of the run, i >= base, in steps of at most 64
-  __device__ __forceinline__ int page(int i, int32_t* err) {
-    if (i - base >= 64) {
-      base += 64;
-      now = next;
-      next = fetch(base + 64, err);
+  __device__ __forceinline__ int64_t of(const AttendArgs& a, const int32_t* table, int len, int h, int first, int i) {
+    if ((i & 63) == 0) {
+      const int page = i == 0 ? fetch(a, table, len, first, 0) : ahead;
+      const int64_t at = place_of<ROW>(a, page, h, first + STRIDE * (i + (int)(threadIdx.x & 63)));
+      lo = (uint32_t)at;
+      hi = (uint32_t)(at >> 32);
+      ahead = fetch(a, table, len, first, i + 64);
     }
-    return __builtin_amdgcn_readlane(now, i - base);
+    return lane_value(lo, hi, i & 63);
   }
 };
-
-// An address that is the same in all lanes, in scalar registers.
-__device__ __forceinline__ const char* uniform(const char* p) {
-  const uint64_t u = (uint64_t)p;
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u);
-  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
-  return reinterpret_cast<const char*>(((uint64_t)hi << 32) | lo);
-}
 
 // ---- where a pair's result goes
 
@@ -298,56 +308,65 @@ struct Geo {
 
 // The loads of 16 keys (of one page) into LDS rows of K or of V: an instruction fills
 // 1 KB, lane i lands on chunk i % CHUNKS of row i / CHUNKS and fetches the chunk that
-// the swizzle puts there.  Keys from the run's end on are zeros.
+// the swizzle puts there.  Keys past a run's end are loaded too (a page is whole), their
+// scores masked and their values cleared (clear_rows).
 template <int D>
 struct Loader {
   using G = Geo<D>;
-  const char* K;               // the key head's part of page 0
-  const char* V;
-  int64_t page_bytes;
-  int shift, page_mask, lr;
   uint32_t ko[G::LOADS], vo;
-  __device__ __forceinline__ void init(const AttendArgs& a, int h) {
-    shift = a.shape.page_shift;
-    page_mask = (1 << shift) - 1;
-    page_bytes = (int64_t)a.shape.kv_heads * G::ROW << shift;
-    K = static_cast<const char*>(a.k_cache) + ((int64_t)h * G::ROW << shift);
-    V = static_cast<const char*>(a.v_cache) + ((int64_t)h * G::ROW << shift);
-    const int lane = threadIdx.x & 63, ch = lane % G::CHUNKS;
-    lr = lane / G::CHUNKS;
+  __device__ __forceinline__ void init() {
+    const int lane = threadIdx.x & 63, ch = lane % G::CHUNKS, lr = lane / G::CHUNKS;
 #pragma unroll
     for (int g = 0; g < G::LOADS; ++g)
       ko[g] = g * 1024 + lr * G::ROW + ((ch ^ G::kswz(G::LOAD_ROWS * g + lr)) << 4);
     vo = lr * G::ROW + ((ch ^ G::vswz(lr)) << 4);
   }
-  template <bool VALUES>
-  __device__ __forceinline__ void load(int page, int key0, int end, char* dst) const {
-    const char* src = uniform((VALUES ? V : K) + page * page_bytes + (int64_t)(key0 & page_mask) * G::ROW);
-    if (key0 + 16 <= end) {
-#pragma unroll
-      for (int g = 0; g < G::LOADS; ++g) lds_dma16(src, VALUES ? vo + g * 1024 : ko[g], dst + g * 1024);
-    } else {
-#pragma unroll
-      for (int g = 0; g < G::LOADS; ++g) {
-        const bool in = key0 + G::LOAD_ROWS * g + lr < end;
-        lds_dma16(in ? (const void*)(src + (VALUES ? vo + g * 1024 : ko[g])) : (const void*)zeros16, dst + g * 1024);
-      }
-    }
+  // load g of the 16 keys (values) from src, the same in all lanes
+  __device__ __forceinline__ void keys(const char* src, uint32_t dst, int g) const { lds_dma16(src, ko[g], dst + g * 1024); }
+  __device__ __forceinline__ void values(const char* src, uint32_t dst, int g) const {
+    lds_dma16(src + g * 1024, vo, dst + g * 1024);
   }
 };
 
-// Whether `rows` rows of V hold a value that is infinite or NaN.
+// Zeros into rows `from` .. 15 of 16 rows.
 template <int D>
-__device__ __forceinline__ bool any_unsound(const char* V, int rows) {
-  bool bad = false;
-#pragma unroll 1
-  for (int c = threadIdx.x & 63; c < rows * Geo<D>::CHUNKS; c += 64) {
-    const uint4 u = *reinterpret_cast<const uint4*>(V + c * 16);
-    const uint32_t v[4] = {u.x, u.y, u.z, u.w};
+__device__ __forceinline__ void clear_rows(char* rows, int from) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) bad |= (v[k] & 0x7f800000u) == 0x7f800000u || (v[k] & 0x7f80u) == 0x7f80u;
+  for (int c = 0; c < 16 * Geo<D>::CHUNKS; c += 64)
+    if (c + lane >= from * Geo<D>::CHUNKS) *reinterpret_cast<uint4*>(rows + (c + lane) * 16) = make_uint4(0, 0, 0, 0);
+}
+
+// The larger magnitudes by their bits; infinite and NaN from 0x7f80 on.
+__device__ __forceinline__ void larger_bits(u16x2_t& m, uint4 u) {
+  const uint32_t v[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2_t, v[k] & 0x7fff7fffu));
+}
+
+// Whether 16 rows of V, in LDS, hold a value that is infinite or NaN.
+template <int D>
+__device__ __forceinline__ bool any_unsound(const char* V) {
+  u16x2_t m = {0, 0};
+#pragma unroll
+  for (int c = 0; c < 16 * Geo<D>::CHUNKS; c += 64)
+    larger_bits(m, *reinterpret_cast<const uint4*>(V + (c + (int)(threadIdx.x & 63)) * 16));
+  return __any(m[0] >= 0x7f80 || m[1] >= 0x7f80);
+}
+
+// Whether the values of tokens from .. to - 1 of a run, which some of the workgroup's pairs
+// see and others do not, hold one: at most as many tokens as the tile has rows.
+template <int D>
+__device__ __forceinline__ bool hidden_unsound(const AttendArgs& a, const int32_t* table, int h, int from, int to) {
+  if (from >= to) return false;
+  u16x2_t m = {0, 0};
+  for (int c = threadIdx.x; c < (to - from) * Geo<D>::CHUNKS; c += 64 * kWaves) {
+    const int key = from + c / Geo<D>::CHUNKS;
+    const int64_t at = place_of<Geo<D>::ROW>(a, checked_page(a, table[key >> a.shape.page_shift]), h, key);
+    larger_bits(m, *reinterpret_cast<const uint4*>(static_cast<const char*>(a.v_cache) + at +
+                                                   c % Geo<D>::CHUNKS * 16));
   }
-  return __any(bad);
+  return __syncthreads_or(m[0] >= 0x7f80 || m[1] >= 0x7f80);
 }
 
 // In a tile, a key that some pairs see and others do not is weighed with 0 for those,
@@ -361,24 +380,26 @@ struct KeyByKey {
   static constexpr int P = 64 / PAIRS;
   f32x4_t o[D / (4 * P)];
   float m, l;
-  __device__ __forceinline__ void start() {
+  int head;
+  __device__ __forceinline__ void start(int h) {
 #pragma unroll
     for (int g = 0; g < D / (4 * P); ++g) o[g] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     m = kLowest;
     l = 0.0f;
+    head = h;
   }
-  __device__ __forceinline__ void add(const AttendArgs& a, const Loader<D>& ld, const int32_t* table,
-                                      const bf16x8_t (&q)[D / (8 * P)], int from, int to, int lim) {
+  __device__ __forceinline__ void add(const AttendArgs& a, const int32_t* table, const bf16x8_t (&q)[D / (8 * P)],
+                                      int from, int to, int lim) {
     const int p = (threadIdx.x & 63) / PAIRS;
 #pragma unroll 1
     for (int key = from; key < to; ++key) {
-      int page = table[key >> ld.shift];
-      if ((uint32_t)page >= (uint32_t)a.shape.pages) page = 0;
-      const int64_t at = page * ld.page_bytes + (int64_t)(key & ld.page_mask) * Geo<D>::ROW;
+      const int64_t at = place_of<Geo<D>::ROW>(a, checked_page(a, table[key >> a.shape.page_shift]), head, key);
+      const char* K = static_cast<const char*>(a.k_cache) + at;
+      const char* V = static_cast<const char*>(a.v_cache) + at;
       float dot = 0.0f;
 #pragma unroll
       for (int s = 0; s < D / (8 * P); ++s) {
-        const bf16x8_t k = *reinterpret_cast<const bf16x8_t*>(ld.K + at + 2 * (8 * P * s + 8 * p));
+        const bf16x8_t k = *reinterpret_cast<const bf16x8_t*>(K + 2 * (8 * P * s + 8 * p));
 #pragma unroll
         for (int j = 0; j < 8; ++j) dot = fmaf((float)q[s][j], (float)k[j], dot);
       }
@@ -390,7 +411,7 @@ struct KeyByKey {
         const float wb = (float)(__bf16)w;
 #pragma unroll
         for (int g = 0; g < D / (4 * P); ++g) {
-          const bf16x4_t v = *reinterpret_cast<const bf16x4_t*>(ld.V + at + 2 * (4 * P * g + 4 * p));
+          const bf16x4_t v = *reinterpret_cast<const bf16x4_t*>(V + 2 * (4 * P * g + 4 * p));
 #pragma unroll
           for (int k = 0; k < 4; ++k) o[g][k] = fmaf(wb, (float)v[k], o[g][k] * f);
         }
@@ -446,18 +467,18 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
   const int lim = live ? sees(a, t, prefix, row) : 0, lim0 = sees(a, t, prefix, t.x0 / r);
 
   Loader<D> ld;
-  ld.init(a, h);
+  ld.init();
   char* ring = smem + wave * SH::STAGES * 2 * SH::BLOCK;
   // block i of the wave: 16 keys from k0 + 16 (wave + 4 i) on
   const int blocks = k1 - k0 > 16 * wave ? (k1 - k0 - 16 * wave + kThinStep - 1) / kThinStep : 0;
-  Window win;
-  if (blocks > 0) win.start(a, t.table, t.len, k0 + 16 * wave);
+  Places<G::ROW, kThinStep> places;
   auto issue = [&](int i) {
-    const int key0 = k0 + 16 * (wave + kWaves * i);
-    char* dst = ring + (i % SH::STAGES) * 2 * SH::BLOCK;
-    const int page = win.page(key0 >> ld.shift, a.err);
-    ld.template load<false>(page, key0, k1, dst);
-    ld.template load<true>(page, key0, k1, dst + SH::BLOCK);
+    const int64_t at = places.of(a, t.table, t.len, h, k0 + 16 * wave, i);
+    const uint32_t dst = (uint32_t)(uintptr_t)(lds_t)ring + (i % SH::STAGES) * 2 * SH::BLOCK;
+#pragma unroll
+    for (int g = 0; g < G::LOADS; ++g) ld.keys(static_cast<const char*>(a.k_cache) + at, dst, g);
+#pragma unroll
+    for (int g = 0; g < G::LOADS; ++g) ld.values(static_cast<const char*>(a.v_cache) + at, dst + SH::BLOCK, g);
   };
   f32x4_t o[D / 16];
 #pragma unroll
@@ -479,8 +500,9 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
     // (a wait alone does not keep the compiler from moving reads of LDS over it)
     asm volatile("" ::: "memory");
     const int kb = k0 + 16 * (wave + kWaves * i);
-    const char* K = ring + (i % SH::STAGES) * 2 * SH::BLOCK;
-    const char* V = K + SH::BLOCK;
+    char* K = ring + (i % SH::STAGES) * 2 * SH::BLOCK;
+    char* V = K + SH::BLOCK;
+    if (kb + 16 > k1) clear_rows<D>(V, k1 - kb);
     f32x4_t st = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) {
@@ -492,7 +514,7 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
       for (int k = 0; k < 4; ++k)
         if (kb + 4 * quad + k >= lim) st[k] = -INFINITY;
       // keys that some pairs see and others do not
-      if (min(kb + 16, k1) > lim0) unsound = unsound || any_unsound<D>(V, 16);
+      if (min(kb + 16, k1) > lim0) unsound = unsound || any_unsound<D>(V);
     }
     const float bm = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3])) * c2;
     if (__any(bm > m + kRescale)) {
@@ -523,10 +545,10 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
   l = quad_sum(l);
   if (unsound) {
     KeyByKey<D, 16> kk;
-    kk.start();
+    kk.start(h);
     for (int i = 0; i < blocks; ++i) {
       const int kb = k0 + 16 * (wave + kWaves * i);
-      kk.add(a, ld, t.table, q, kb, min(kb + 16, k1), lim);
+      kk.add(a, t.table, q, kb, min(kb + 16, k1), lim);
     }
     m = kk.m;
     l = kk.l;
@@ -595,44 +617,69 @@ struct Pairs {
   float m, l;             // m is the pair's, l this lane's share
 };
 
-// Scores of 64 keys in the LDS tile K.
+// Values that are to be there at this place of the instruction order: the compiler
+// otherwise moves what makes them to where they are used.
+template <typename A>
+__device__ __forceinline__ void pin(A& a) { asm volatile("" : "+v"(a)); }
+template <typename A, typename B>
+__device__ __forceinline__ void pin(A& a, B& b) { asm volatile("" : "+v"(a), "+v"(b)); }
+
+// Fragments of a step's 64 keys in LDS: K's k-th operand is 32 keys 32 (k % 2) .. of
+// elements 16 (k / 2) ..; V^T's is 32 elements 32 (k % (D / 32)) .. of 16 keys
+// 16 (k / (D / 32)) .., in the order in which a lane holds the probabilities: slot
+// 8 (l / 32) + j is key 4 (l / 32) + j for j < 4 and 8 + 4 (l / 32) + j - 4 for j >= 4.  It
+// is read from the row-major tile by the transposing LDS read: 16 lanes read four keys
+// x 16 columns, lane i receives column i of the four.
+//
+// The swizzles act on address bits that the operands' own offsets reach by exclusive or,
+// so each lane keeps one address for K and one for V (key_lane, value_lane, from the
+// step's first byte), and an operand costs one instruction.
 template <int D>
-__device__ __forceinline__ void scores(const Pairs<D>& w, const char* K, f32x16_t (&st)[2]) {
-  using G = Geo<D>;
+__device__ __forceinline__ uint32_t key_lane() {
   const int lane = threadIdx.x & 63, ql = lane & 31, half = lane >> 5;
-#pragma unroll
-  for (int n = 0; n < 2; ++n)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) st[n][i] = 0.0f;
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s)
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      const uint4 u = *reinterpret_cast<const uint4*>(K + (32 * n + ql) * G::ROW +
-                                                      (((2 * s + half) ^ G::kswz(ql)) << 4));
-      st[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, u), w.q[s], st[n], 0, 0, 0);
-    }
+  return ql * Geo<D>::ROW + ((half ^ Geo<D>::kswz(ql)) << 4);
+}
+template <int D>
+__device__ __forceinline__ uint32_t value_lane() {
+  const int lane = threadIdx.x & 63, vr = (lane >> 2) & 3;
+  return (4 * (lane >> 5) + vr) * Geo<D>::ROW + (Geo<D>::vswz(vr) << 4) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+}
+template <int D>
+__device__ __forceinline__ bf16x8_t key_operand(uint32_t K, int k) {
+  typedef const __attribute__((address_space(3))) bf16x8_t* ptr_t;
+  return *(ptr_t)(lds_t)(uintptr_t)((K ^ (k >> 1) << 5) + 32 * (k & 1) * Geo<D>::ROW);
+}
+template <int D>
+__device__ __forceinline__ bf16x8_t value_operand(uint32_t V, int k) {
+  const lds_t p = (lds_t)(uintptr_t)((V ^ (k % (D / 32)) << 6) + 16 * (k / (D / 32)) * Geo<D>::ROW);
+  const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((ltr_t)p);
+  const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((ltr_t)(p + 8 * Geo<D>::ROW));
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// Hides keys from `lim` on (counted in the tile).
+// Hides keys from `lim` on (counted in the step).
 __device__ __forceinline__ void hide(f32x16_t (&st)[2], int lim) {
-  const int half = (threadIdx.x & 63) >> 5;
+  const int from = lim - 4 * (int)((threadIdx.x & 63) >> 5);
 #pragma unroll
   for (int n = 0; n < 2; ++n)
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-      if (32 * n + 8 * (i >> 2) + 4 * half + (i & 3) >= lim) st[n][i] = -INFINITY;
+      if (32 * n + 8 * (i >> 2) + (i & 3) >= from) st[n][i] = -INFINITY;
 }
 
-// The running maximum moves, and the sums are rescaled, only when a score exceeds it
-// by more than 2^8, which float32 sums hold with the same relative error.
-template <int D>
-__device__ __forceinline__ void move_max(Pairs<D>& w, const f32x16_t (&st)[2], float c2) {
+__device__ __forceinline__ float largest(const f32x16_t (&st)[2]) {
   float bm = st[0][0];
 #pragma unroll
   for (int n = 0; n < 2; ++n)
 #pragma unroll
     for (int i = 0; i < 16; ++i) bm = fmaxf(bm, st[n][i]);
+  return bm;
+}
+
+// The running maximum moves, and the sums are rescaled, only when a score exceeds it
+// by more than 2^8, which float32 sums hold with the same relative error.
+template <int D>
+__device__ __forceinline__ void move_max(Pairs<D>& w, float bm, float c2) {
   bm *= c2;
   if (__any(bm > w.m + kRescale)) {
     const float mn = fmaxf(w.m, half_max(bm));
@@ -646,41 +693,85 @@ __device__ __forceinline__ void move_max(Pairs<D>& w, const f32x16_t (&st)[2], f
   }
 }
 
+// Weighs scores 2 e and 2 e + 1 of the 32 that a lane holds.
 template <int D>
-__device__ __forceinline__ void weights(Pairs<D>& w, const f32x16_t (&st)[2], bf16x8_t (&pb)[4], float c2) {
-#pragma unroll
-  for (int n = 0; n < 2; ++n)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float p = __builtin_amdgcn_exp2f(fmaf(st[n][i], c2, -w.m));
-      w.l += p;
-      pb[2 * n + (i >> 3)][i & 7] = (__bf16)p;
-    }
+__device__ __forceinline__ void weigh(Pairs<D>& w, const f32x16_t (&st)[2], bf16x8_t (&pb)[4], int e, float c2) {
+  const float p0 = __builtin_amdgcn_exp2f(fmaf(st[e >> 3][2 * (e & 7)], c2, -w.m));
+  const float p1 = __builtin_amdgcn_exp2f(fmaf(st[e >> 3][2 * (e & 7) + 1], c2, -w.m));
+  w.l += p0;
+  w.l += p1;
+  bf16x2_t b = {(__bf16)p0, (__bf16)p1};
+  pin(w.l, b);
+  pb[e >> 2][2 * (e & 3)] = b[0];
+  pb[e >> 2][2 * (e & 3) + 1] = b[1];
 }
 
-// The probabilities a lane holds are its half of the operand's k slots as they stand:
-// slot 8 (l / 32) + j is key 4 (l / 32) + j for j < 4 and 8 + 4 (l / 32) + j - 4 for
-// j >= 4.  The value operand is read from the row-major tile by the transposing LDS
-// read: 16 lanes read four keys x 16 columns, lane i receives column i of the four.
-template <int D>
-__device__ __forceinline__ void add_values(Pairs<D>& w, const char* V, const bf16x8_t (&pb)[4]) {
-  using G = Geo<D>;
-  const int lane = threadIdx.x & 63, vr = (lane >> 2) & 3;
-  const char* base = V + (4 * (lane >> 5) + vr) * G::ROW + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+// One step: weighs its scores st and adds its values V, while (NEXT) the next step's
+// scores are made of its keys K, into st, and their largest is returned.  The matrix
+// cores and the vector units work at the same time only where their instructions
+// alternate, and a product waits for its operand's LDS read unless that was issued
+// well before; so the order is written down: operands four products ahead, and between
+// the products the step's loads (issue) and the 16 pairs of scores, 10 of them beside the next scores, 6 beside the
+// values of the first 32 keys.  (In the compiler's order 1.17 ms for 8 prompts of 3840
+// rows, 28 heads of 128 on 4.)
+template <int D, bool NEXT, typename Issue>
+__device__ __forceinline__ float pipeline_step(Pairs<D>& w, f32x16_t (&st)[2], uint32_t K, uint32_t V, float c2,
+                                               Issue issue) {
+  constexpr int N = D / 8, AHEAD = 4, BESIDE = NEXT ? 10 : 0;      // products of each kind
+  bf16x8_t kf[AHEAD], vf[AHEAD], pb[4];
+  f32x16_t nx[2];
+  pin(K, V);                                       // (else every operand's address is kept in a register)
+  if constexpr (NEXT) {
 #pragma unroll
-  for (int g = 0; g < 4; ++g)
+    for (int k = 0; k < AHEAD; ++k) kf[k] = key_operand<D>(K, k);
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t) {
-      const int piece = (4 * t ^ G::vswz(vr)) << 4;
-      const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((ltr_t)(base + piece + 16 * g * G::ROW));
-      const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((ltr_t)(base + piece + (16 * g + 8) * G::ROW));
-      const bf16x8_t v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      w.o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pb[g], w.o[t], 0, 0, 0);
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) nx[n][i] = 0.0f;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      nx[k & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k % AHEAD], w.q[k >> 1], nx[k & 1], 0, 0, 0);
+      if (k + AHEAD < N) kf[k % AHEAD] = key_operand<D>(K, k + AHEAD);
+      else vf[k + AHEAD - N] = value_operand<D>(V, k + AHEAD - N);
+      issue(k);
+#pragma unroll
+      for (int e = k * BESIDE / N; e < (k + 1) * BESIDE / N; ++e) weigh(w, st, pb, e, c2);
+      __builtin_amdgcn_sched_barrier(0);
     }
+  } else {
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) vf[k] = value_operand<D>(V, k);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) weigh(w, st, pb, e, c2);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  constexpr int DONE = NEXT ? BESIDE : 8;
+  float bm = kLowest;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    w.o[k % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k % AHEAD], pb[k / (D / 32)], w.o[k % (D / 32)], 0, 0, 0);
+    if (k + AHEAD < N) vf[k % AHEAD] = value_operand<D>(V, k + AHEAD);
+    if (k < N / 2) {
+#pragma unroll
+      for (int e = DONE + k * (16 - DONE) * 2 / N; e < DONE + (k + 1) * (16 - DONE) * 2 / N; ++e) weigh(w, st, pb, e, c2);
+    } else if constexpr (NEXT) {
+#pragma unroll
+      for (int e = (k - N / 2) * 64 / N; e < (k + 1 - N / 2) * 64 / N; e += 2)
+        bm = fmaxf(fmaxf(bm, nx[e >> 4][e & 15]), nx[e >> 4][(e & 15) + 1]);
+      pin(bm);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if constexpr (NEXT) {
+    st[0] = nx[0];
+    st[1] = nx[1];
+  }
+  return bm;
 }
 
-// 128 pairs, 32 a wave; the waves share tiles of 64 keys, K and V two deep each.  While
-// the vector units weigh one tile's scores, the next tile's are on the matrix cores.
+// 128 pairs, 32 a wave; the waves share steps of 64 keys, K and V two deep each.  While
+// the vector units weigh one step's scores, the next step's are on the matrix cores.
 // Keys: a fused tile takes its prefix's steps first (the last one may be ragged), then
 // its own run's.
 template <int D>
@@ -707,6 +798,10 @@ __device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool 
   const int xw = t.x0 + 32 * wave, x = xw + ql;
   const bool idle = xw >= t.pairs;                                            // the wave has no pair
   const bool live = x < t.pairs;
+  // a tile whose sequences all take the prefix by themselves
+  if (prefix && a.rows.max_rows * (int64_t)r > kFuse &&
+      !__syncthreads_or(live && prefix_place(a, t, h, x, chunk).pair >= 0))
+    return;
   const int row = live ? x / r : 0;
   Pairs<D> w;
   const uint16_t* qsrc =
@@ -726,74 +821,119 @@ __device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool 
   const int lim = live ? sees(a, t, prefix, row) : 0, lim0 = idle ? 0 : sees(a, t, prefix, xw / r);
   const float c2 = a.c2;
 
-  // the wave loads keys 16 wave .. of every step: one page
+  // The wave loads keys 16 wave .. of every step, which lie in one page.  Lane j holds
+  // where those of step 64 (i / 64) + j are, and the page of 64 steps on.
   Loader<D> ld;
-  ld.init(a, h);
-  int32_t* const err = a.err;
-  Window kw, vw, own;
-  if (v0 < before) {
-    kw.start(a, a.prefix.table + (int64_t)g * a.prefix.width, P, v0 * kTallStep);
-    own.start(a, t.table, t.len, 0);
-  } else {
-    kw.start(a, t.table, t.len, (v0 - before) * kTallStep);
-    own = kw;
-  }
-  vw = kw;
-  auto issue = [&](auto values, Window& win, int i) {
-    constexpr bool VALUES = decltype(values)::value;
-    const int v = v0 + i;
-    if (v == before && i > 0) win = own;
-    const int key0 = (v < before ? v : v - before) * kTallStep + 16 * wave;
-    ld.template load<VALUES>(win.page(key0 >> ld.shift, err), key0, v < before ? P : end,
-                             smem + ((VALUES ? 2 : 0) + (i & 1)) * STEP + 16 * wave * G::ROW);
+  ld.init();
+  auto fetch = [&](int i) {
+    const AttendArgs& f = arguments();
+    const int v = v0 + i + lane;
+    const bool p = v < before;
+    const int key = (p ? v : v - before) * kTallStep + 16 * wave;
+    int page = 0;
+    if (key < (p ? P : t.len)) page = pages_of(f, prefix || p, p ? g : t.seg)[key >> f.shape.page_shift];
+    return checked_page(f, page);
   };
-  // keys of step i that the lane's pair sees, counted in the step; the wave's first pair; all
-  auto seen = [&](int i, int of_run) { return v0 + i < before ? P - (v0 + i) * kTallStep
-                                                              : of_run - (v0 + i - before) * kTallStep; };
+  uint32_t at_lo = 0, at_hi = 0;
+  int ahead = 0;
+  auto place = [&](int i) {
+    if ((i & 63) == 0) {
+      const int v = v0 + i + lane;
+      const int64_t at = place_of<G::ROW>(arguments(), i == 0 ? fetch(0) : ahead, h,
+                                          (v < before ? v : v - before) * kTallStep + 16 * wave);
+      at_lo = (uint32_t)at;
+      at_hi = (uint32_t)(at >> 32);
+      ahead = fetch(i + 64);
+    }
+    return lane_value(at_lo, at_hi, i & 63);
+  };
+  // operand addresses of even steps
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_t)smem;
+  const uint32_t kl = lds0 + key_lane<D>(), vl = lds0 + 2 * STEP + value_lane<D>();
+  const char* const Kc = static_cast<const char*>(a.k_cache);
+  const char* const Vc = static_cast<const char*>(a.v_cache);
+  const uint32_t mine = lds0 + 16 * wave * G::ROW;   // the wave's rows of a step
+  // Steps that end inside a step's keys: the prefix's last, the run's last.  From step
+  // `masked` on the wave's first pair does not see all keys.
+  const int ragged = P % kTallStep ? before - 1 - v0 : -1, last = end % kTallStep ? before - v0 + end / kTallStep : -1;
+  const int masked = before - v0 + lim0 / kTallStep;
+  // before step i's values are used: those past the end are cleared
+  auto clear = [&](int i) {
+    const int left = (i == ragged ? P : end) % kTallStep - 16 * wave;
+    if (left < 16) clear_rows<D>(smem + (2 + (i & 1)) * STEP + 16 * wave * G::ROW, left < 0 ? 0 : left);
+    __syncthreads();
+  };
+  // keys of step i that the lane's pair sees
+  auto mask = [&](f32x16_t (&st)[2], int i) {
+    if (i == ragged) hide(st, P % kTallStep);
+    else hide(st, lim - (v0 + i - before) * kTallStep);
+  };
   bool unsound = false;
   if (n > 0) {
-    issue(std::false_type{}, kw, 0);
-    issue(std::true_type{}, vw, 0);
-    if (n > 1) issue(std::false_type{}, kw, 1);
+    int64_t at = place(0);
+#pragma unroll
+    for (int k = 0; k < G::LOADS; ++k) ld.keys(Kc + at, mine, k);
+#pragma unroll
+    for (int k = 0; k < G::LOADS; ++k) ld.values(Vc + at, mine + 2 * STEP, k);
+    at = place(1);
+#pragma unroll
+    for (int k = 0; k < G::LOADS; ++k) ld.keys(Kc + at, mine + STEP, k);
+    unsound = hidden_unsound<D>(a, t.table, h, max(sees(a, t, prefix, t.x0 / r), (v0 - before) * kTallStep),
+                                min(end, (v0 + n - before) * kTallStep));
     f32x16_t st[2];
     wait_vmcnt<0>();
     __syncthreads();
     if (!idle) {
-      scores(w, smem, st);
-      if (seen(0, lim0) < kTallStep) hide(st, seen(0, lim));
-      move_max(w, st, c2);
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) st[m][e] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < D / 8; ++k)
+        st[k & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_operand<D>(kl, k), w.q[k >> 1], st[k & 1], 0, 0, 0);
+      if (0 == ragged || 0 >= masked) mask(st, 0);
+      move_max(w, largest(st), c2);
     }
-    for (int i = 0; i < n; ++i) {
+    for (int i = 0; i < n - 1; ++i) {
       wait_vmcnt<0>();                               // this wave's loads of K i + 1 and V i
       __syncthreads();                               // every wave's; and all are past K i and V i - 1
-      if (i + 2 < n) issue(std::false_type{}, kw, i + 2);
-      if (i + 1 < n) issue(std::true_type{}, vw, i + 1);
-      if (idle) continue;
-      const char* V = smem + (2 + (i & 1)) * STEP;
-      // keys that some pairs of the wave see and others do not
-      if (min(seen(i, end), kTallStep) > max(seen(i, lim0), 0)) unsound = unsound || any_unsound<D>(V, kTallStep);
-      bf16x8_t pb[4];
-      f32x16_t nx[2];
-      if (i + 1 < n) scores(w, smem + ((i + 1) & 1) * STEP, nx);
-      weights(w, st, pb, c2);
-      add_values(w, V, pb);
-      if (i + 1 < n) {
-        if (seen(i + 1, lim0) < kTallStep) hide(nx, seen(i + 1, lim));
-        move_max(w, nx, c2);
+      if (i == ragged || i == last) clear(i);
+      // the loads of V i + 1 and K i + 2 (whether or not there is such a step: nothing reads it then)
+      const char* vs = Vc + at;
+      at = place(i + 2);
+      const char* ks = Kc + at;
+      const int odd = i & 1;
+      auto issue = [&](int k) {
+        if (k < G::LOADS) ld.values(vs, mine + (3 - odd) * STEP, k);
+        else if (k < 2 * G::LOADS) ld.keys(ks, mine + odd * STEP, k - G::LOADS);
+      };
+      if (idle) {
+#pragma unroll
+        for (int k = 0; k < 2 * G::LOADS; ++k) issue(k);
+        continue;
       }
-      st[0] = nx[0];
-      st[1] = nx[1];
+      float bm = pipeline_step<D, true>(w, st, kl + (1 - odd) * STEP, vl + odd * STEP, c2, issue);
+      if (i + 1 == ragged || i + 1 >= masked) {
+        mask(st, i + 1);
+        bm = largest(st);
+      }
+      move_max(w, bm, c2);
     }
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (n - 1 == ragged || n - 1 == last) clear(n - 1);
+    if (!idle) pipeline_step<D, false>(w, st, 0, vl + ((n - 1) & 1) * STEP, c2, [](int) {});
   }
   w.l = half_sum(w.l);
   if (unsound) {
+    const AttendArgs& f = arguments();
     KeyByKey<D, 32> kk;
-    kk.start();
+    kk.start(h);
     for (int i = 0; i < n; ++i) {
       const bool p = v0 + i < before;
       const int kb = (p ? v0 + i : v0 + i - before) * kTallStep;
-      kk.add(a, ld, p ? a.prefix.table + (int64_t)g * a.prefix.width : t.table, w.q, kb,
-             min(kb + kTallStep, p ? P : end), p ? P : lim);
+      kk.add(f, pages_of(f, prefix || p, p ? g : t.seg), w.q, kb, min(kb + kTallStep, p ? P : end),
+             p ? P : lim);
     }
     w.m = kk.m;
     w.l = kk.l;
@@ -804,29 +944,30 @@ __device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool 
   }
 
   if (!live) return;
+  const AttendArgs& e = arguments();
   const int row_steps = before + ceil_div(lim, kTallStep);
-  const Out u = prefix ? prefix_place(a, t, h, x, chunk) : own_place(a, t, h, x, chunk, ceil_div(row_steps, chunk_steps), pre);
+  const Out u = prefix ? prefix_place(e, t, h, x, chunk) : own_place(e, t, h, x, chunk, ceil_div(row_steps, chunk_steps), pre);
   if (u.pair < 0) return;
-  if (half == 0) store_ml(a, u, w.m, w.l);
+  if (half == 0) store_ml(e, u, w.m, w.l);
   if (u.done) {
     const float inv = w.l == 0.0f ? 0.0f : 1.0f / w.l;
-    __bf16* dst = static_cast<__bf16*>(a.O) + u.pair * D + 4 * half;
+    __bf16* dst = static_cast<__bf16*>(e.O) + u.pair * D + 4 * half;
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e)
+    for (int b = 0; b < D / 32; ++b)
 #pragma unroll
       for (int g4 = 0; g4 < 4; ++g4) {
         bf16x4_t v;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = (__bf16)(w.o[e][4 * g4 + k] * inv);
-        *reinterpret_cast<bf16x4_t*>(dst + 32 * e + 8 * g4) = v;
+        for (int k = 0; k < 4; ++k) v[k] = (__bf16)(w.o[b][4 * g4 + k] * inv);
+        *reinterpret_cast<bf16x4_t*>(dst + 32 * b + 8 * g4) = v;
       }
   } else {
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e)
+    for (int b = 0; b < D / 32; ++b)
 #pragma unroll
       for (int g4 = 0; g4 < 4; ++g4)
-        *reinterpret_cast<float4*>(u.o + 32 * e + 8 * g4 + 4 * half) =
-            make_float4(w.o[e][4 * g4], w.o[e][4 * g4 + 1], w.o[e][4 * g4 + 2], w.o[e][4 * g4 + 3]);
+        *reinterpret_cast<float4*>(u.o + 32 * b + 8 * g4 + 4 * half) =
+            make_float4(w.o[b][4 * g4], w.o[b][4 * g4 + 1], w.o[b][4 * g4 + 2], w.o[b][4 * g4 + 3]);
   }
 }
 
@@ -849,6 +990,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a) {
     const bool prefix = tall == 1;
     if (!prefix) id -= p.prefix_blocks;
     const int tiles = prefix ? p.prefix_tiles : p.tall_tiles;
+    // Workgroup w runs on XCD w % 8: 32 tiles that follow one another, and so mostly share
+    // their keys, on each in turn.
+    if ((id | 255) < (prefix ? p.prefix_blocks : p.tall_blocks)) id = (id & ~255) + (id % 8) * 32 + id / 8 % 32;
     const int rest = id / tiles, tile = tiles - 1 - (id - rest * tiles);
     if (!find_tile<kTall>(a, prefix, tile, t)) return;
     if (!prefix && t.pairs <= kThin) return;                                 // a thin tile's
@@ -923,16 +1067,13 @@ __global__ __launch_bounds__(64 * kWaves) void attend_f32_kernel(AttendArgs a) {
 #pragma unroll
   for (int e = 0; e < D / 16; ++e) o[e] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   float m = kLowest, l = 0.0f;
-  const int page_mask = (1 << a.shape.page_shift) - 1;
   const int blocks = k1 - k0 > 16 * wave ? (k1 - k0 - 16 * wave + 16 * kWaves - 1) / (16 * kWaves) : 0;
-  Window win;
-  if (blocks > 0) win.start(a, t.table, t.len, k0 + 16 * wave);
+  Places<4 * D, kThinStep> places;
   for (int i = 0; i < blocks; ++i) {
     const int kb = k0 + 16 * (wave + kWaves * i);
-    const int64_t head_page = (int64_t)win.page(kb >> a.shape.page_shift, a.err) * a.shape.kv_heads + h;
-    const int64_t at = (head_page * (page_mask + 1) + (kb & page_mask)) * D;
-    const float* K = static_cast<const float*>(a.k_cache) + at;
-    const float* V = static_cast<const float*>(a.v_cache) + at;
+    const int64_t at = places.of(a, t.table, t.len, h, k0 + 16 * wave, i);
+    const float* K = reinterpret_cast<const float*>(static_cast<const char*>(a.k_cache) + at);
+    const float* V = reinterpret_cast<const float*>(static_cast<const char*>(a.v_cache) + at);
     const int in = k1 - kb;                          // keys of the block
     f32x4_t k[D / 16];
 #pragma unroll

@@ -33,6 +33,13 @@ __device__ __forceinline__ void lds_dma16(const char* base, uint32_t off, char* 
                :: "v"(off), "s"(base), "s"(l) : "memory", "m0");
 }
 
+// The same into the LDS byte address `dst`, uniform in the wave.
+__device__ __forceinline__ void lds_dma16(const char* base, uint32_t off, uint32_t dst) {
+  const uint32_t l = __builtin_amdgcn_readfirstlane(dst);
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               :: "v"(off), "s"(base), "s"(l) : "memory", "m0");
+}
+
 // s_waitcnt with only the vector-memory counter constrained (gfx9 encoding).
 template <int N>
 __device__ __forceinline__ void wait_vmcnt() {
