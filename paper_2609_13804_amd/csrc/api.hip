@@ -178,7 +178,7 @@ struct AttendWs {
 };
 AttendWs attend_ws_layout(const AttendArgs& a) {
   const AttendPlan& p = a.plan;
-  const size_t brief = (size_t)a.runs.count * p.short_rows * a.shape.q_heads;
+  const size_t brief = (size_t)short_slots(a);
   const bool joined = p.prefix_parts > 0 || p.short_parts > 1;
   const size_t n[3] = {joined ? brief * p.short_parts : 0, brief * p.prefix_parts,
                        p.tall_parts > 1 ? (size_t)a.rows.rows * a.shape.q_heads * p.tall_parts : 0};

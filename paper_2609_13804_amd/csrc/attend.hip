@@ -24,6 +24,7 @@
 //                     reads saves nothing and parts would only be written and read.
 #include <float.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "sp_internal.h"
@@ -36,6 +37,7 @@ namespace {
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
@@ -135,14 +137,16 @@ __device__ __forceinline__ int sees(const AttendArgs& a, const Tile& t, bool pre
   return v < 0 ? 0 : (int)v;
 }
 
-// The group of sequence s and the tokens of its prefix: 0 without one.
-__device__ __forceinline__ int prefix_of(const AttendArgs& a, int s, int& g) {
-  g = 0;
-  if (a.prefix.count == 0) return 0;
-  g = wave_find_last(a.prefix.count, s, [&](int i) { return a.grp_off[i]; });
-  int len;
-  if (s < a.grp_off[g] || s >= a.grp_off[g + 1] || tokens_of(a.prefix, g, len) != SP_DEV_OK) return 0;
-  return len;
+// The group of sequence s: -1 without one.
+__device__ __forceinline__ int group_of(const AttendArgs& a, int s) {
+  if (a.prefix.count == 0) return -1;
+  const int g = wave_find_last(a.prefix.count, s, [&](int i) { return a.grp_off[i]; });
+  return s < a.grp_off[g] || s >= a.grp_off[g + 1] ? -1 : g;
+}
+
+// The tokens of its prefix.  (`len` is the prefixes' entry: loaded ahead of its use)
+__device__ __forceinline__ int prefix_tokens(const AttendArgs& a, int g, int len) {
+  return g < 0 || len < 0 || len > a.prefix.max_len ? 0 : len;
 }
 
 __device__ __forceinline__ const int32_t* pages_of(const AttendArgs& a, bool prefix, int i) {
@@ -170,23 +174,35 @@ __device__ __forceinline__ int64_t lane_value(uint32_t lo, uint32_t hi, int from
   return (int64_t)((uint64_t)h << 32 | l);
 }
 
-// Places of the 16-key blocks that a wave takes, one every STRIDE keys from `first` on:
+// Places of the 16-key blocks that a wave takes, one every `stride` keys from `first` on:
 // lane j holds that of block 64 (i / 64) + j, and the page of the block 64 further on.
-template <int ROW, int STRIDE>
+// The pages' loads need no length (prime can go ahead of the loads of the batch's
+// entries): entries past the run's tokens are read, within the table, and not used.
+template <int ROW>
 struct Places {
+  const int32_t* table;
+  int first, stride, width;
   uint32_t lo, hi;
   int ahead;
-  __device__ __forceinline__ int fetch(const AttendArgs& a, const int32_t* table, int len, int first, int i) const {
-    const int key = first + STRIDE * (i + (int)(threadIdx.x & 63));
-    return checked_page(a, key < len ? table[key >> a.shape.page_shift] : 0);
+  __device__ __forceinline__ int entry(const AttendArgs& a, int i) const {
+    const int64_t at = (first + (int64_t)stride * (i + (int)(threadIdx.x & 63))) >> a.shape.page_shift;
+    return at < width ? table[at] : 0;
   }
-  __device__ __forceinline__ int64_t of(const AttendArgs& a, const int32_t* table, int len, int h, int first, int i) {
+  __device__ __forceinline__ void prime(const AttendArgs& a, const CacheRuns& runs, int run, int key, int step) {
+    table = runs.table + (int64_t)run * runs.width;
+    width = runs.width;
+    first = key;
+    stride = step;
+    ahead = entry(a, 0);
+  }
+  // of block i, asked for in order
+  __device__ __forceinline__ int64_t of(const AttendArgs& a, int len, int h, int i) {
     if ((i & 63) == 0) {
-      const int page = i == 0 ? fetch(a, table, len, first, 0) : ahead;
-      const int64_t at = place_of<ROW>(a, page, h, first + STRIDE * (i + (int)(threadIdx.x & 63)));
+      const int64_t key = first + (int64_t)stride * (i + (int)(threadIdx.x & 63));
+      const int64_t at = place_of<ROW>(a, checked_page(a, key < len ? ahead : 0), h, (int)key);
       lo = (uint32_t)at;
       hi = (uint32_t)(at >> 32);
-      ahead = fetch(a, table, len, first, i + 64);
+      ahead = entry(a, i + 64);
     }
     return lane_value(lo, hi, i & 63);
   }
@@ -204,8 +220,11 @@ struct Out {
 // Sequences of up to this many pairs are short: their parts lie by sequence.
 __device__ __forceinline__ bool is_short(const AttendArgs& a, int pairs) { return pairs <= a.plan.short_pairs; }
 
-__device__ __forceinline__ int64_t short_base(const AttendArgs& a, int s, int row_of_seq) {
-  return ((int64_t)s * a.plan.short_rows + row_of_seq) * a.shape.q_heads;
+// Where the parts of row i of sequence s, row `row` of the batch, begin: by row where all
+// sequences are short (its sequence need not be known then), else by sequence (the rows of
+// the long ones would leave large gaps).
+__device__ __forceinline__ int64_t short_base(const AttendArgs& a, int64_t row, int s, int i) {
+  return (a.plan.by_row ? row : (int64_t)s * a.plan.short_rows + i) * a.shape.q_heads;
 }
 
 // Pair x of sequence t.seg and key head h: the place of its result over chunk `chunk` of
@@ -222,7 +241,7 @@ __device__ __forceinline__ Out own_place(const AttendArgs& a, const Tile& t, int
   u.pair = row * a.shape.q_heads + head;
   int64_t at;
   if (is_short(a, t.pairs)) {
-    at = (short_base(a, t.seg, i) + head) * a.plan.short_parts + chunk;
+    at = (short_base(a, row, t.seg, i) + head) * a.plan.short_parts + chunk;
     u.o = a.short_o;
     u.ml = reinterpret_cast<float2*>(a.short_ml);
   } else {
@@ -243,25 +262,25 @@ __device__ __forceinline__ Out prefix_place(const AttendArgs& a, const Tile& t, 
   u.done = false;
   const int r = ratio(a), j = x / r, head = h * r + (x - j * r);
   const int64_t row = t.row0 + j;
-  int s, i, n;
+  int s = 0, i = 0;
   if (a.rows.padded) {
     s = (int)(row / a.rows.rows_per_seq);
     i = (int)(row - (int64_t)s * a.rows.rows_per_seq);
-    n = a.rows.info[s];
-  } else {                                           // info[s] <= row < info[s + 1]
+    const int n = a.rows.info[s];
+    if (i >= n || n > a.rows.max_rows || (int64_t)n * r > a.plan.short_pairs) return u;
+  } else if (!a.plan.by_row) {                       // info[s] <= row < info[s + 1]
     s = a.grp_off[t.seg];
     for (int hi = a.grp_off[t.seg + 1]; hi - s > 1;) {
       const int mid = (s + hi) >> 1;
       if (a.rows.info[mid] <= row) s = mid;
       else hi = mid;
     }
-    const int first = a.rows.info[s];
+    const int first = a.rows.info[s], n = a.rows.info[s + 1] - first;
     i = (int)(row - first);
-    n = a.rows.info[s + 1] - first;
+    if (i < 0 || i >= n || n > a.rows.max_rows || (int64_t)n * r > a.plan.short_pairs) return u;
   }
-  if (i < 0 || i >= n || n > a.rows.max_rows || (int64_t)n * r > a.plan.short_pairs) return u;
   u.pair = row * a.shape.q_heads + head;
-  const int64_t at = (short_base(a, s, i) + head) * a.plan.prefix_parts + chunk;
+  const int64_t at = (short_base(a, row, s, i) + head) * a.plan.prefix_parts + chunk;
   u.o = a.prefix_o + at * a.shape.head_dim;
   u.ml = reinterpret_cast<float2*>(a.prefix_ml) + at;
   return u;
@@ -338,20 +357,9 @@ __device__ __forceinline__ void clear_rows(char* rows, int from) {
 }
 
 // The larger magnitudes by their bits; infinite and NaN from 0x7f80 on.
-__device__ __forceinline__ void larger_bits(u16x2_t& m, uint4 u) {
-  const uint32_t v[4] = {u.x, u.y, u.z, u.w};
+__device__ __forceinline__ void larger_bits(u16x2_t& m, u32x4_t v) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2_t, v[k] & 0x7fff7fffu));
-}
-
-// Whether 16 rows of V, in LDS, hold a value that is infinite or NaN.
-template <int D>
-__device__ __forceinline__ bool any_unsound(const char* V) {
-  u16x2_t m = {0, 0};
-#pragma unroll
-  for (int c = 0; c < 16 * Geo<D>::CHUNKS; c += 64)
-    larger_bits(m, *reinterpret_cast<const uint4*>(V + (c + (int)(threadIdx.x & 63)) * 16));
-  return __any(m[0] >= 0x7f80 || m[1] >= 0x7f80);
 }
 
 // Whether the values of tokens from .. to - 1 of a run, which some of the workgroup's pairs
@@ -363,8 +371,8 @@ __device__ __forceinline__ bool hidden_unsound(const AttendArgs& a, const int32_
   for (int c = threadIdx.x; c < (to - from) * Geo<D>::CHUNKS; c += 64 * kWaves) {
     const int key = from + c / Geo<D>::CHUNKS;
     const int64_t at = place_of<Geo<D>::ROW>(a, checked_page(a, table[key >> a.shape.page_shift]), h, key);
-    larger_bits(m, *reinterpret_cast<const uint4*>(static_cast<const char*>(a.v_cache) + at +
-                                                   c % Geo<D>::CHUNKS * 16));
+    larger_bits(m, *reinterpret_cast<const u32x4_t*>(static_cast<const char*>(a.v_cache) + at +
+                                                     c % Geo<D>::CHUNKS * 16));
   }
   return __syncthreads_or(m[0] >= 0x7f80 || m[1] >= 0x7f80);
 }
@@ -424,28 +432,34 @@ constexpr int kAttendLds = 64 * 1024;      // two workgroups to a compute unit
 
 // ---------------------------------------------------------------- the thin tiles
 
-// 16 pairs; each of four waves takes every fourth block of 16 keys through a ring of its
-// own in LDS (no barrier until the end), and the waves' results are joined through
-// LDS.  Scores S^T = K Q^T and O^T += V^T P as in the tall tiles, with 16 x 16
-// matrices: lane l holds pair l % 16, scores of keys 4 (l / 16) + i, output elements
-// 16 t + 4 (l / 16) + i.
+// 16 pairs.  The keys of one head go to all four waves, each every fourth block of 16, and
+// the waves' results are joined through LDS; or (spread) each wave takes a head of its own.  Scores S^T = K Q^T and O^T += V^T P as in the tall tiles, with
+// 16 x 16 matrices: lane l holds pair l % 16, scores of keys 4 (l / 16) + i, output
+// elements 16 t + 4 (l / 16) + i.
+//
+// Bound by memory.  Three blocks are in registers or on their way there (24 KB a wave,
+// 192 KB a compute unit): K in the operand's layout as it comes, V to be transposed
+// through 4 KB of LDS a wave.  So a workgroup alone keeps its compute unit's share of the
+// bandwidth while its neighbour starts or ends.  (With rings of two blocks in LDS, filled
+// directly: 128 single tokens of 256 to 8192 keys, 28 heads on 4, 219 us.)
 template <int D>
 struct ThinShape {
   static constexpr int BLOCK = 16 * Geo<D>::ROW;                // 16 keys of K or V
-  static constexpr int STAGES = kAttendLds / (kWaves * 2 * BLOCK);
   static constexpr int PART_ROW = D + 4;
-  static_assert(kWaves * kThin * (PART_ROW + 2) * 4 <= kAttendLds, "the waves' results fit the rings");
+  static constexpr int DEPTH = 2;
+  static_assert(2 * kWaves * BLOCK <= kAttendLds && kWaves * kThin * (PART_ROW + 2) * 4 <= kAttendLds,
+                "the blocks, then the waves' results, fit the LDS");
 };
 
 template <int D>
-__device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool prefix, const Tile& t, int h, int chunk) {
+__device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool prefix, const Tile& t,
+                                          Places<Geo<D>::ROW>& places, int h, int chunk, int g, bool spread) {
   using G = Geo<D>;
   using SH = ThinShape<D>;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ql = lane & 15, quad = lane >> 4, r = ratio(a);
   const int chunk_keys = prefix ? a.plan.chunk_prefix : a.plan.chunk_thin;
-  int g;
-  const int pre = prefix ? 0 : ceil_div(prefix_of(a, t.seg, g), a.plan.chunk_prefix);
+  const int prefix_len = prefix || g < 0 ? 0 : a.prefix.len[g];    // (used at the end)
   // the last pair's limit is the tile's
   const int tile_end = sees(a, t, prefix, (min(t.x0 + kThin, t.pairs) - 1) / r);
   const int k0 = chunk * chunk_keys;
@@ -466,19 +480,22 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
   }
   const int lim = live ? sees(a, t, prefix, row) : 0, lim0 = sees(a, t, prefix, t.x0 / r);
 
-  Loader<D> ld;
-  ld.init();
-  char* ring = smem + wave * SH::STAGES * 2 * SH::BLOCK;
-  // block i of the wave: 16 keys from k0 + 16 (wave + 4 i) on
-  const int blocks = k1 - k0 > 16 * wave ? (k1 - k0 - 16 * wave + kThinStep - 1) / kThinStep : 0;
-  Places<G::ROW, kThinStep> places;
-  auto issue = [&](int i) {
-    const int64_t at = places.of(a, t.table, t.len, h, k0 + 16 * wave, i);
-    const uint32_t dst = (uint32_t)(uintptr_t)(lds_t)ring + (i % SH::STAGES) * 2 * SH::BLOCK;
+  // block i of the wave: 16 keys from first + step i on
+  const int first = places.first, step = places.stride;
+  const int blocks = k1 > first ? (k1 - first + step - 1) / step : 0;
+  const char* const Kc = static_cast<const char*>(a.k_cache);
+  const char* const Vc = static_cast<const char*>(a.v_cache);
+  struct Block {
+    u32x4_t k[G::LOADS], v[G::LOADS];
+  };
+  // No load is left out (the waits count them): past the last block all lanes load one place.
+  auto load = [&](Block& b, int i) {
+    const int64_t at = places.of(a, t.len, h, i);
+    const uint32_t mine = i < blocks ? lane * 16 : 0, next = i < blocks ? 1024 : 0;
 #pragma unroll
-    for (int g = 0; g < G::LOADS; ++g) ld.keys(static_cast<const char*>(a.k_cache) + at, dst, g);
+    for (int c = 0; c < G::LOADS; ++c) b.k[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(Kc + at + c * next + mine));
 #pragma unroll
-    for (int g = 0; g < G::LOADS; ++g) ld.values(static_cast<const char*>(a.v_cache) + at, dst + SH::BLOCK, g);
+    for (int c = 0; c < G::LOADS; ++c) b.v[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(Vc + at + c * next + mine));
   };
   f32x4_t o[D / 16];
 #pragma unroll
@@ -486,36 +503,41 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
   float m = kLowest, l = 0.0f;
   bool unsound = false;
   const float c2 = a.c2;
-#pragma unroll
-  for (int i = 0; i < SH::STAGES - 1; ++i)
-    if (i < blocks) issue(i);
-  for (int i = 0; i < blocks; ++i) {
-    if (i + SH::STAGES - 1 < blocks) {
-      wait_lgkm0();                                  // the reads of the buffer that is filled next
-      issue(i + SH::STAGES - 1);
-      wait_vmcnt<(SH::STAGES - 1) * 2 * G::LOADS>();
-    } else {
-      wait_vmcnt<0>();
-    }
-    // (a wait alone does not keep the compiler from moving reads of LDS over it)
-    asm volatile("" ::: "memory");
-    const int kb = k0 + 16 * (wave + kWaves * i);
-    char* K = ring + (i % SH::STAGES) * 2 * SH::BLOCK;
-    char* V = K + SH::BLOCK;
-    if (kb + 16 > k1) clear_rows<D>(V, k1 - kb);
+  // LDS addresses: K, then V.  Row LOAD_ROWS c + lr of K has chunk ch at ch ^ kswz of the row,
+  // in which c and lr set bits apart; V^T's read: 16 lanes read four keys x 16 columns, lane
+  // i receives column i of the four keys.
+  const uint32_t K = (uint32_t)(uintptr_t)(lds_t)smem + wave * 2 * SH::BLOCK, V = K + SH::BLOCK;
+  const int lr = lane / G::CHUNKS, ch = lane % G::CHUNKS, vr = (lane >> 2) & 3;
+  const uint32_t kdst = K + lr * G::ROW + ((ch ^ G::kswz(lr)) << 4);
+  const uint32_t ksrc = K + ql * G::ROW + ((quad ^ G::kswz(ql)) << 4);
+  const uint32_t vdst = V + lr * G::ROW + ((ch ^ G::vswz(lr)) << 4);
+  const uint32_t vsrc = V + (4 * quad + vr) * G::ROW + (G::vswz(vr) << 4) + (lane & 3) * 8;
+  typedef __attribute__((address_space(3))) u32x4_t* l16_t;
+  auto use = [&](Block& b, int i) {
+    const int kb = first + step * i;
     f32x4_t st = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int s = 0; s < D / 32; ++s) {
-      const uint4 u = *reinterpret_cast<const uint4*>(K + ql * G::ROW + (((4 * s + quad) ^ G::kswz(ql)) << 4));
-      st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, u), q[s], st, 0, 0, 0);
-    }
+    for (int c = 0; c < G::LOADS; ++c)
+      *(l16_t)(lds_t)(uintptr_t)((kdst ^ G::kswz(G::LOAD_ROWS * c) << 4) + c * 1024) = b.k[c];
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s)
+      st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+          __builtin_bit_cast(bf16x8_t, *(l16_t)(lds_t)(uintptr_t)(ksrc ^ s << 6)), q[s], st, 0, 0, 0);
     if (kb + 16 > lim0) {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         if (kb + 4 * quad + k >= lim) st[k] = -INFINITY;
-      // keys that some pairs see and others do not
-      if (min(kb + 16, k1) > lim0) unsound = unsound || any_unsound<D>(V);
+      // past the end: zeros; keys that some pairs see and others do not: looked at
+#pragma unroll
+      for (int c = 0; c < G::LOADS; ++c)
+        if (kb + G::LOAD_ROWS * c + lr >= k1) b.v[c] = u32x4_t{0, 0, 0, 0};
+      u16x2_t bits = {0, 0};
+#pragma unroll
+      for (int c = 0; c < G::LOADS; ++c) larger_bits(bits, b.v[c]);
+      if (min(kb + 16, k1) > lim0) unsound = unsound || __any(bits[0] >= 0x7f80 || bits[1] >= 0x7f80);
     }
+#pragma unroll
+    for (int c = 0; c < G::LOADS; ++c) *(l16_t)(lds_t)(uintptr_t)(vdst + c * 1024) = b.v[c];
     const float bm = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3])) * c2;
     if (__any(bm > m + kRescale)) {
       const float mn = fmaxf(m, quad_max(bm));
@@ -532,14 +554,23 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
       l += p;
       pb[k] = (__bf16)p;
     }
-    // V^T: 16 lanes read four keys x 16 columns, lane i receives column i of the four keys
-    const int vr = (lane >> 2) & 3, vrow = 4 * quad + vr;
 #pragma unroll
     for (int e = 0; e < D / 16; ++e) {
-      const bf16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-          (ltr_t)(V + vrow * G::ROW + (((2 * e) ^ G::vswz(vr)) << 4) + (lane & 3) * 8));
+      const bf16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((ltr_t)(lds_t)(uintptr_t)(vsrc ^ e << 5));
       o[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, v), __builtin_bit_cast(s16x4_t, pb),
                                                        o[e], 0, 0, 0);
+    }
+  };
+  if (blocks > 0) {
+    Block b[SH::DEPTH];
+#pragma unroll
+    for (int j = 0; j < SH::DEPTH; ++j) load(b[j], j);
+    for (int i = 0; i < blocks; i += SH::DEPTH) {
+#pragma unroll
+      for (int j = 0; j < SH::DEPTH; ++j) {
+        if (i + j < blocks) use(b[j], i + j);
+        load(b[j], i + j + SH::DEPTH);
+      }
     }
   }
   l = quad_sum(l);
@@ -547,13 +578,34 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
     KeyByKey<D, 16> kk;
     kk.start(h);
     for (int i = 0; i < blocks; ++i) {
-      const int kb = k0 + 16 * (wave + kWaves * i);
+      const int kb = first + step * i;
       kk.add(a, t.table, q, kb, min(kb + 16, k1), lim);
     }
     m = kk.m;
     l = kk.l;
 #pragma unroll
     for (int e = 0; e < D / 16; ++e) o[e] = kk.o[e];
+  }
+
+  const int pre = ceil_div(prefix_tokens(a, g, prefix_len), a.plan.chunk_prefix);
+  if (spread) {
+    if (!live) return;
+    const Out u = own_place(a, t, h, x, chunk, ceil_div(lim, chunk_keys), pre);
+    if (u.pair < 0) return;
+    if (quad == 0) store_ml(a, u, m, l);
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) {
+      if (u.done) {
+        bf16x4_t v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = (__bf16)(o[e][k] * inv);
+        *reinterpret_cast<bf16x4_t*>(static_cast<__bf16*>(a.O) + u.pair * D + 16 * e + 4 * quad) = v;
+      } else {
+        *reinterpret_cast<f32x4_t*>(u.o + 16 * e + 4 * quad) = o[e];
+      }
+    }
+    return;
   }
 
   // the waves' results, joined: part [wave][pair][PART_ROW], then [m, l][wave][pair]
@@ -780,9 +832,10 @@ __device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool 
   constexpr int STEP = kTallStep * G::ROW;                                    // 64 keys of K or V
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ql = lane & 31, half = lane >> 5, r = ratio(a);
-  int g, pre = 0, P = 0;                             // parts of the prefix apart; its tokens taken here
+  int g = -1, pre = 0, P = 0;                        // parts of the prefix apart; its tokens taken here
   if (!prefix) {
-    P = prefix_of(a, t.seg, g);
+    g = group_of(a, t.seg);
+    P = prefix_tokens(a, g, g < 0 ? 0 : a.prefix.len[g]);
     if (t.pairs <= kFuse) {
       pre = ceil_div(P, a.plan.chunk_prefix);
       P = 0;
@@ -1002,19 +1055,27 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a) {
   const bool prefix = id < p.prefix_blocks;
   if (!prefix) id -= p.prefix_blocks + p.tall_blocks;
   const int tiles = prefix ? p.prefix_tiles : a.runs.count;
-  const int rest = id / tiles, tile = id - rest * tiles;
+  const bool spread = !prefix && p.spread;
+  const int per = spread ? heads / kWaves : heads, rest = id / tiles, tile = id - rest * tiles, chunk = rest / per;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int h = spread ? (rest - chunk * per) * kWaves + wave : rest - chunk * per;
+  Places<Geo<D>::ROW> places;
+  int g = -1;
   if (prefix) {
     if (!find_tile<kThin>(a, true, tile, t)) return;
+    places.prime(a, a.prefix, t.seg, chunk * p.chunk_prefix + 16 * wave, kThinStep);
   } else {                                           // a sequence to a tile; longer ones are the tall tiles'
     t.seg = tile;
-    if (rows_of(a.rows, t.seg, t.row0, t.n) != SP_DEV_OK) return;
+    places.prime(a, a.runs, t.seg, chunk * p.chunk_thin + (spread ? 0 : 16 * wave), spread ? 16 : kThinStep);
+    const int tokens = tokens_of(a.runs, t.seg, t.len), rows = rows_of(a.rows, t.seg, t.row0, t.n);
+    g = group_of(a, t.seg);
     const int64_t pairs = (int64_t)t.n * ratio(a);
-    if (pairs == 0 || pairs > kThin || tokens_of(a.runs, t.seg, t.len) != SP_DEV_OK) return;
+    if (rows != SP_DEV_OK || tokens != SP_DEV_OK || pairs == 0 || pairs > kThin) return;
     t.pairs = (int)pairs;
     t.x0 = 0;
     t.table = a.runs.table + (int64_t)t.seg * a.runs.width;
   }
-  thin_tile<D>(a, smem, prefix, t, rest % heads, rest / heads);
+  thin_tile<D>(a, smem, prefix, t, places, h, chunk, g, spread);
 }
 
 // ---------------------------------------------------------------- float32
@@ -1042,8 +1103,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_f32_kernel(AttendArgs a) {
   Tile t;
   if (!find_tile<kThin>(a, prefix, id - rest * tiles, t)) return;
   const int chunk_keys = prefix ? a.plan.chunk_prefix : a.plan.chunk_thin;
-  int gi;
-  const int pre = prefix ? 0 : ceil_div(prefix_of(a, t.seg, gi), a.plan.chunk_prefix);
+  const int g = prefix ? -1 : group_of(a, t.seg), prefix_len = g < 0 ? 0 : a.prefix.len[g];
   const int r = ratio(a);
   const int tile_end = sees(a, t, prefix, (min(t.x0 + kThin, t.pairs) - 1) / r);
   const int k0 = chunk * chunk_keys;
@@ -1068,10 +1128,11 @@ __global__ __launch_bounds__(64 * kWaves) void attend_f32_kernel(AttendArgs a) {
   for (int e = 0; e < D / 16; ++e) o[e] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   float m = kLowest, l = 0.0f;
   const int blocks = k1 - k0 > 16 * wave ? (k1 - k0 - 16 * wave + 16 * kWaves - 1) / (16 * kWaves) : 0;
-  Places<4 * D, kThinStep> places;
+  Places<4 * D> places;
+  places.prime(a, prefix ? a.prefix : a.runs, t.seg, k0 + 16 * wave, kThinStep);
   for (int i = 0; i < blocks; ++i) {
     const int kb = k0 + 16 * (wave + kWaves * i);
-    const int64_t at = places.of(a, t.table, t.len, h, k0 + 16 * wave, i);
+    const int64_t at = places.of(a, t.len, h, i);
     const float* K = reinterpret_cast<const float*>(static_cast<const char*>(a.k_cache) + at);
     const float* V = reinterpret_cast<const float*>(static_cast<const char*>(a.v_cache) + at);
     const int in = k1 - kb;                          // keys of the block
@@ -1159,6 +1220,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_f32_kernel(AttendArgs a) {
   const int c = tid >> 4, e0 = (tid & 15) * E;
   const int xc = t.x0 + c;
   if (xc >= t.pairs) return;
+  const int pre = ceil_div(prefix_tokens(a, g, prefix_len), a.plan.chunk_prefix);
   const Out u = prefix ? prefix_place(a, t, h, xc, chunk)
                        : own_place(a, t, h, xc, chunk, ceil_div(sees(a, t, false, xc / r), chunk_keys), pre);
   if (u.pair < 0) return;
@@ -1197,14 +1259,16 @@ __global__ __launch_bounds__(64 * kWaves) void combine_kernel(AttendArgs a, int 
   const AttendPlan& p = a.plan;
   int64_t row = -1, base = 0;                        // the row's parts from pair `base` on
   const int head = (int)(at % Hq);
-  if (tall) {
+  if (tall || p.by_row) {
     row = at / Hq;
     base = row * Hq;
     bool live = row < a.rows.rows;
     if (live && a.rows.padded) {
       const int64_t s = row / a.rows.rows_per_seq;
       live = s < a.runs.count && row - s * a.rows.rows_per_seq < a.rows.info[s] &&
-             a.rows.info[s] * (int64_t)ratio(a) > p.short_pairs;
+             (!tall || a.rows.info[s] * (int64_t)ratio(a) > p.short_pairs);
+    } else if (live && !tall) {
+      live = row >= a.rows.info[0] && row < a.rows.info[a.runs.count];
     } else if (live) {
       const int s = wave_find_last(a.runs.count, row, [&](int i) { return (int64_t)a.rows.info[i]; });
       live = row >= a.rows.info[s] && row < a.rows.info[s + 1] &&
@@ -1219,7 +1283,7 @@ __global__ __launch_bounds__(64 * kWaves) void combine_kernel(AttendArgs a, int 
       const int i = (int)((at - s * per) / Hq);
       if (i < n && (int64_t)n * ratio(a) <= p.short_pairs) {
         row = first + i;
-        base = short_base(a, (int)s, i);
+        base = short_base(a, row, (int)s, i);
       }
     }
   }
@@ -1297,16 +1361,20 @@ __global__ __launch_bounds__(64 * kWaves) void combine_kernel(AttendArgs a, int 
   if (a.lse && lane == 0) a.lse[out] = lse_of(M, L);
 }
 
-// Keys of a chunk: enough chunks that `items` tiles and key heads give the device about
-// `target` workgroups, of at least `least` keys each, in whole steps.
-inline int chunk_of(int64_t items, int64_t max_len, int64_t target, int least, int step) {
-  int64_t parts = (target + items - 1) / items;
-  const int64_t most = (max_len + least - 1) / least;
-  if (parts > most) parts = most;
-  if (parts > kMaxParts) parts = kMaxParts;
-  if (parts < 1) parts = 1;
-  const int64_t keys = (max_len + parts - 1) / parts;
-  return (int)((keys + step - 1) / step * step) + (keys == 0 ? step : 0);
+// Keys of a chunk, in whole steps, for `items` tiles and key heads: chunks of at least
+// `least` keys until the device's 512 places for workgroups have one each, then of at
+// least `more` keys until there are four for each, which evens out unequal lengths.
+// (us: one run of 131001 tokens, 4 key heads, in 512 parts of 256 / 128 of 1024 64 / 56;
+// 128 ragged runs of up to 8192 tokens, 4 key heads, in chunks of 8192 / 2048 / 1024
+// 229 / 218 / 229: every workgroup costs a few us to begin and to end.)
+inline int chunk_of(int64_t items, int64_t max_len, int least, int more, int step) {
+  auto ceil64 = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
+  if (items < 1) items = 1;
+  const int64_t fill = std::min(ceil64(512, items), ceil64(max_len, least));
+  const int64_t even = std::min(ceil64(2048, items), ceil64(max_len, more));
+  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(kMaxParts, std::max(fill, even)));
+  const int64_t keys = ceil64(max_len, parts);
+  return (int)std::max<int64_t>(step, ceil64(keys, step) * step);
 }
 
 inline int parts_of(int64_t max_len, int chunk) { return (int)((max_len + chunk - 1) / chunk); }
@@ -1323,15 +1391,19 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
   // float32 has no tall tiles: every sequence is short, and its prefix is shared
   p.short_pairs = (int)(f32 || longest < kFuse ? longest : kFuse);
   if (p.short_pairs < 1) p.short_pairs = 1;
+  p.by_row = longest <= p.short_pairs;
   p.short_rows = (int)((p.short_pairs + r - 1) / r);
   p.thin_tiles = (int)(f32 ? pairs / kThin + S : S);
-  p.chunk_thin = chunk_of((p.thin_tiles > 0 ? p.thin_tiles : 1) * heads, runs.max_len, 2048, 256, kThinStep);
-  p.thin_blocks = p.thin_tiles * heads * (runs.max_len > 0 ? parts_of(runs.max_len, p.chunk_thin) : 1);
+  // a wave to a head where there are enough heads for all waves of the device
+  p.spread = !f32 && heads % kWaves == 0 && S * heads >= 2048;
+  const int64_t units = p.spread ? heads / kWaves : heads;
+  p.chunk_thin = chunk_of((f32 ? std::max(S, pairs / kThin) : S) * units, runs.max_len, 256, 2048, kThinStep);
+  p.thin_blocks = p.thin_tiles * units * (runs.max_len > 0 ? parts_of(runs.max_len, p.chunk_thin) : 1);
   p.short_parts = parts_of(runs.max_len, p.chunk_thin);
   if (own_tall) {
     const int64_t keys = (prefix.max_len + kTallStep - 1) / kTallStep * kTallStep + (int64_t)runs.max_len;
     p.tall_tiles = (int)(pairs / kTall + S);
-    p.chunk_tall = chunk_of((p.tall_tiles > 0 ? p.tall_tiles : 1) * heads, keys, 512, 512, kTallStep);
+    p.chunk_tall = chunk_of(std::max(S, pairs / kTall) * heads, keys, 512, INT_MAX, kTallStep);
     p.tall_parts = parts_of(keys, p.chunk_tall);
     p.tall_blocks = p.tall_tiles * heads * (p.tall_parts > 0 ? p.tall_parts : 1);
     if (p.tall_parts > p.short_parts) p.short_parts = p.tall_parts;
@@ -1339,8 +1411,9 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
   if (G > 0 && prefix.max_len > 0) {
     p.prefix_tall = !f32 && pairs > kThin * G;
     p.prefix_tiles = (int)(pairs / (p.prefix_tall ? kTall : kThin) + G);
-    p.chunk_prefix = p.prefix_tall ? chunk_of(p.prefix_tiles * heads, prefix.max_len, 512, 512, kTallStep)
-                                   : chunk_of(p.prefix_tiles * heads, prefix.max_len, 2048, 256, kThinStep);
+    p.chunk_prefix = p.prefix_tall
+                         ? chunk_of(std::max(G, pairs / kTall) * heads, prefix.max_len, 512, INT_MAX, kTallStep)
+                         : chunk_of(std::max(G, pairs / kThin) * heads, prefix.max_len, 256, 2048, kThinStep);
     p.prefix_parts = parts_of(prefix.max_len, p.chunk_prefix);
     p.prefix_blocks = p.prefix_tiles * heads * p.prefix_parts;
   } else {
@@ -1370,8 +1443,7 @@ void launch_attend(const AttendArgs& a, hipStream_t stream) {
   else
     hipLaunchKernelGGL(attend_kernel<D>, grid, block, 0, stream, a);
   if (p.prefix_parts > 0 || p.short_parts > 1)
-    launch_combine<T, D>(a, (int64_t)a.runs.count * p.short_rows * a.shape.q_heads, p.prefix_parts + p.short_parts, 0,
-                         stream);
+    launch_combine<T, D>(a, short_slots(a), p.prefix_parts + p.short_parts, 0, stream);
   if (p.tall_parts > 1 && a.rows.max_rows * (int64_t)(a.shape.q_heads / a.shape.kv_heads) > p.short_pairs)
     launch_combine<T, D>(a, a.rows.rows * a.shape.q_heads, p.tall_parts, 1, stream);
 }

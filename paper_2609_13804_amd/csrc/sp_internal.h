@@ -217,7 +217,9 @@ struct AttendPlan {
   int chunk_prefix, chunk_thin, chunk_tall;         // keys of a chunk
   int prefix_parts, short_parts, tall_parts;        // most parts of a row: over its prefix, its own keys
   int short_pairs, short_rows;                      // the largest short sequence's pairs, rows
+  int by_row;                                       // all are short: their parts lie by row, not by sequence
   int prefix_tall;                                  // the prefixes' tiles are tall ones
+  int spread;                                       // thin tiles: a wave to a key head, not four
   int prefix_tiles, tall_tiles, thin_tiles;         // tiles of a key head
   int64_t prefix_blocks, tall_blocks, thin_blocks;  // workgroups
 };
@@ -238,16 +240,20 @@ struct AttendArgs {
   AttendPlan plan;
   // workspace pieces
   int2* row_parts;        // [rows]: parts over the row's own keys (0: it is done), over its prefix
-  float* short_ml;        // short sequences: [count, short_rows, q_heads, short_parts, 2]
-  float* short_o;         //                  [count, short_rows, q_heads, short_parts, head_dim]
-  float* prefix_ml;       // their prefixes:  [count, short_rows, q_heads, prefix_parts, 2]
-  float* prefix_o;        //                  [count, short_rows, q_heads, prefix_parts, head_dim]
+  float* short_ml;        // short sequences: [rows or count short_rows, q_heads, short_parts, 2]
+  float* short_o;         //                  [.., q_heads, short_parts, head_dim]
+  float* prefix_ml;       // their prefixes:  [.., q_heads, prefix_parts, 2]
+  float* prefix_o;        //                  [.., q_heads, prefix_parts, head_dim]
   float* tall_ml;         // the others:      [rows, q_heads, tall_parts, 2]
   float* tall_o;          //                  [rows, q_heads, tall_parts, head_dim]
   int32_t* err;
 };
 AttendPlan plan_cache_attend(const CacheShape& shape, const CacheRows& rows, const CacheRuns& runs,
                              const CacheRuns& prefix);
+// (row, head) pairs whose parts the short sequences' arrays hold.
+inline int64_t short_slots(const AttendArgs& a) {
+  return (a.plan.by_row ? a.rows.rows : (int64_t)a.runs.count * a.plan.short_rows) * a.shape.q_heads;
+}
 hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t stream);
 
 // C = A B^T for bfloat16 A [M, K] and B [N, K] (rows K-contiguous), bfloat16

@@ -85,6 +85,19 @@ def test_large_groups(gpu_lib, D, per_group):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_wave_to_a_head(gpu_lib, dtype):
+    """So many sequences and key heads that each wave takes a head by itself; lengths from
+    none to several chunks, some rows in groups."""
+    S = 40
+    lens = [(37 * s) % 90 for s in range(S)]
+    lens[3], lens[11] = 2200, 300
+    b = Batch([1 + (s % 7 == 0) for s in range(S)], lens, heads=(64, 64), D=64, dtype=dtype, prefix=[50, 333],
+              cuts=[2, 20, 31], seed=13)
+    b.upload()
+    b.check(*b.attend())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_cross_attention(gpu_lib, dtype):
     """Runs of no token at all: every row attends to its group's prefix alone."""
     b = Batch([20, 3, 50], [0, 0, 0], heads=(4, 4), D=64, dtype=dtype, prefix=[77, 300], cuts=[0, 1, 2], seed=3)
