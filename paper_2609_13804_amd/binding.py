@@ -159,10 +159,24 @@ def _events(events):
     return ctypes.cast(arr, ctypes.c_void_p)
 
 
+_current = None
+
+
+def _current_stream() -> int:
+    """torch's current stream on the current device, as a raw handle.  A stream object
+    costs 2.9 us a call, a third of a small call; torch's own handle query 0.3 us."""
+    global _current
+    if _current is None:
+        import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _current = ((lambda: raw(torch.cuda.current_device())) if raw is not None else
+                    (lambda: torch.cuda.current_stream().cuda_stream))
+    return _current()
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

@@ -609,6 +609,7 @@ sp_status stepprune_cache_attend(const sp_cache_dims* dims, const void* Q, int64
   a.Q = Q;
   a.ldq = ldq;
   a.c2 = c2;
+  a.c2_low = (float)((double)scale * 1.4426950408889634 - (double)c2);
   a.all = (flags & SP_ATTEND_ALL) != 0;
   a.k_cache = k_cache;
   a.v_cache = v_cache;

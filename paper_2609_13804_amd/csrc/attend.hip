@@ -64,6 +64,20 @@ __device__ __forceinline__ const AttendArgs& arguments() {
   return *(const AttendArgs*)p;
 }
 
+// 16 bytes of a type.
+template <typename T>
+struct Chunk;
+template <>
+struct Chunk<__bf16> {
+  static constexpr int N = 8;
+  typedef bf16x8_t vec;
+};
+template <>
+struct Chunk<float> {
+  static constexpr int N = 4;
+  typedef f32x4_t vec;
+};
+
 // ---------------------------------------------------------------- tiles
 
 struct Tile {
@@ -295,7 +309,7 @@ __device__ __forceinline__ void store_ml(const AttendArgs& a, const Out& u, floa
   else if (a.lse) a.lse[u.pair] = lse_of(m, l);
 }
 
-// ---------------------------------------------------------------- bfloat16
+// ---------------------------------------------------------------- operands
 
 __device__ __forceinline__ float half_max(float v) {      // of this lane and the lane 32 away
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -356,10 +370,13 @@ __device__ __forceinline__ void clear_rows(char* rows, int from) {
     if (c + lane >= from * Geo<D>::CHUNKS) *reinterpret_cast<uint4*>(rows + (c + lane) * 16) = make_uint4(0, 0, 0, 0);
 }
 
-// The larger magnitudes by their bits; infinite and NaN from 0x7f80 on.
+// The larger magnitudes by the bits of their upper halves (bfloat16: of both halves of
+// four bytes); infinite and NaN from 0x7f80 on.
+template <typename T>
 __device__ __forceinline__ void larger_bits(u16x2_t& m, u32x4_t v) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2_t, v[k] & 0x7fff7fffu));
+  for (int k = 0; k < 4; ++k)
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2_t, v[k] & (sizeof(T) == 2 ? 0x7fff7fffu : 0x7fff0000u)));
 }
 
 // Whether the values of tokens from .. to - 1 of a run, which some of the workgroup's pairs
@@ -371,8 +388,8 @@ __device__ __forceinline__ bool hidden_unsound(const AttendArgs& a, const int32_
   for (int c = threadIdx.x; c < (to - from) * Geo<D>::CHUNKS; c += 64 * kWaves) {
     const int key = from + c / Geo<D>::CHUNKS;
     const int64_t at = place_of<Geo<D>::ROW>(a, checked_page(a, table[key >> a.shape.page_shift]), h, key);
-    larger_bits(m, *reinterpret_cast<const u32x4_t*>(static_cast<const char*>(a.v_cache) + at +
-                                                     c % Geo<D>::CHUNKS * 16));
+    larger_bits<__bf16>(m, *reinterpret_cast<const u32x4_t*>(static_cast<const char*>(a.v_cache) + at +
+                                                             c % Geo<D>::CHUNKS * 16));
   }
   return __syncthreads_or(m[0] >= 0x7f80 || m[1] >= 0x7f80);
 }
@@ -381,11 +398,13 @@ __device__ __forceinline__ bool hidden_unsound(const AttendArgs& a, const int32_
 // which is NaN where its value is infinite or NaN.  A wave that meets one begins again
 // here, key by key, each pair over the keys that it sees alone (a hundred times slower,
 // and never needed by sound data).  Lane l holds pair l % PAIRS; with p = l / PAIRS of P
-// lanes a pair, elements 8 P s + 8 p + 0 .. 7 of its query in q[s] and 4 P g + 4 p + 0 .. 3
-// of its output in o[g].
-template <int D, int PAIRS>
+// lanes a pair and E elements in 16 bytes, elements E (P s + p) + 0 .. E - 1 of its query
+// in q[s] and 4 (P g + p) + 0 .. 3 of its output in o[g].
+template <typename T, int D, int PAIRS>
 struct KeyByKey {
-  static constexpr int P = 64 / PAIRS;
+  using vec = typename Chunk<T>::vec;
+  typedef T vec4 __attribute__((ext_vector_type(4)));
+  static constexpr int P = 64 / PAIRS, E = Chunk<T>::N;
   f32x4_t o[D / (4 * P)];
   float m, l;
   int head;
@@ -396,32 +415,33 @@ struct KeyByKey {
     l = 0.0f;
     head = h;
   }
-  __device__ __forceinline__ void add(const AttendArgs& a, const int32_t* table, const bf16x8_t (&q)[D / (8 * P)],
+  __device__ __forceinline__ void add(const AttendArgs& a, const int32_t* table, const vec (&q)[D / (E * P)],
                                       int from, int to, int lim) {
     const int p = (threadIdx.x & 63) / PAIRS;
 #pragma unroll 1
     for (int key = from; key < to; ++key) {
-      const int64_t at = place_of<Geo<D>::ROW>(a, checked_page(a, table[key >> a.shape.page_shift]), head, key);
+      const int64_t at =
+          place_of<D * (int)sizeof(T)>(a, checked_page(a, table[key >> a.shape.page_shift]), head, key);
       const char* K = static_cast<const char*>(a.k_cache) + at;
       const char* V = static_cast<const char*>(a.v_cache) + at;
       float dot = 0.0f;
 #pragma unroll
-      for (int s = 0; s < D / (8 * P); ++s) {
-        const bf16x8_t k = *reinterpret_cast<const bf16x8_t*>(K + 2 * (8 * P * s + 8 * p));
+      for (int s = 0; s < D / (E * P); ++s) {
+        const vec k = *reinterpret_cast<const vec*>(K + 16 * (P * s + p));
 #pragma unroll
-        for (int j = 0; j < 8; ++j) dot = fmaf((float)q[s][j], (float)k[j], dot);
+        for (int j = 0; j < E; ++j) dot = fmaf((float)q[s][j], (float)k[j], dot);
       }
       const float sc = (P == 2 ? half_sum(dot) : quad_sum(dot)) * a.c2;
       if (key < lim) {
         const float mn = fmaxf(m, sc), f = __builtin_amdgcn_exp2f(m - mn), w = __builtin_amdgcn_exp2f(sc - mn);
         m = mn;
         l = fmaf(l, f, w);
-        const float wb = (float)(__bf16)w;
+        const float wt = (float)(T)w;
 #pragma unroll
         for (int g = 0; g < D / (4 * P); ++g) {
-          const bf16x4_t v = *reinterpret_cast<const bf16x4_t*>(V + 2 * (4 * P * g + 4 * p));
+          const vec4 v = *reinterpret_cast<const vec4*>(V + sizeof(vec4) * (P * g + p));
 #pragma unroll
-          for (int k = 0; k < 4; ++k) o[g][k] = fmaf(wb, (float)v[k], o[g][k] * f);
+          for (int k = 0; k < 4; ++k) o[g][k] = fmaf(wt, (float)v[k], o[g][k] * f);
         }
       }
     }
@@ -433,29 +453,34 @@ constexpr int kAttendLds = 64 * 1024;      // two workgroups to a compute unit
 // ---------------------------------------------------------------- the thin tiles
 
 // 16 pairs.  The keys of one head go to all four waves, each every fourth block of 16, and
-// the waves' results are joined through LDS; or (spread) each wave takes a head of its own.  Scores S^T = K Q^T and O^T += V^T P as in the tall tiles, with
-// 16 x 16 matrices: lane l holds pair l % 16, scores of keys 4 (l / 16) + i, output
-// elements 16 t + 4 (l / 16) + i.
+// the waves' results are joined through LDS; or (spread) each wave takes a head of its own.
+// Scores S^T = K Q^T and O^T += V^T P as in the tall tiles, with 16 x 16 matrices: lane l
+// holds pair l % 16, scores of keys 4 (l / 16) + i, output elements 16 t + 4 (l / 16) + i.
 //
-// Bound by memory.  Three blocks are in registers or on their way there (24 KB a wave,
-// 192 KB a compute unit): K in the operand's layout as it comes, V to be transposed
-// through 4 KB of LDS a wave.  So a workgroup alone keeps its compute unit's share of the
-// bandwidth while its neighbour starts or ends.  (With rings of two blocks in LDS, filled
-// directly: 128 single tokens of 256 to 8192 keys, 28 heads on 4, 219 us.)
-template <int D>
+// Bound by memory.  Two blocks are in registers or on their way there, K and V in whole
+// 1 KB loads; through LDS they come into the operands' layouts.  They are read once, so
+// they are not kept in the caches: 128 single tokens of 256 to 8192 keys, 28 heads on 4,
+// 204 us (5.3 TB/s), with ordinary loads 225, and three blocks ahead 207; 64 of 8192 keys
+// 178 us (6.0 TB/s).
+template <typename T, int D>
 struct ThinShape {
-  static constexpr int BLOCK = 16 * Geo<D>::ROW;                // 16 keys of K or V
+  static constexpr int ROW = D * (int)sizeof(T), CHUNKS = ROW / 16, LOAD_ROWS = 1024 / ROW, LOADS = 16 / LOAD_ROWS;
+  // LDS rows: bfloat16 as in the tall tiles; float32 padded by 16 bytes, so that 16 rows'
+  // chunks (K), and four rows' runs of 16 elements (V), touch every bank once
+  static constexpr int LDS_ROW = sizeof(T) == 2 ? ROW : ROW + 16;
+  static constexpr int BLOCK = 16 * LDS_ROW;                    // 16 keys of K or V
   static constexpr int PART_ROW = D + 4;
   static constexpr int DEPTH = 2;
-  static_assert(2 * kWaves * BLOCK <= kAttendLds && kWaves * kThin * (PART_ROW + 2) * 4 <= kAttendLds,
-                "the blocks, then the waves' results, fit the LDS");
+  static constexpr int BLOCKS = 2 * kWaves * BLOCK, PARTS = kWaves * kThin * (PART_ROW + 2) * 4;
+  static constexpr int LDS = BLOCKS > PARTS ? BLOCKS : PARTS;   // the blocks, then the waves' results
 };
 
-template <int D>
+template <typename T, int D>
 __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool prefix, const Tile& t,
-                                          Places<Geo<D>::ROW>& places, int h, int chunk, int g, bool spread) {
-  using G = Geo<D>;
-  using SH = ThinShape<D>;
+                                          Places<D * (int)sizeof(T)>& places, int h, int chunk, int g, bool spread) {
+  using SH = ThinShape<T, D>;
+  using vec = typename Chunk<T>::vec;
+  constexpr int E = Chunk<T>::N, QS = D / (4 * E);               // query vectors of a lane
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ql = lane & 15, quad = lane >> 4, r = ratio(a);
   const int chunk_keys = prefix ? a.plan.chunk_prefix : a.plan.chunk_thin;
@@ -469,14 +494,13 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
   const int x = t.x0 + ql;
   const bool live = x < t.pairs;
   const int row = live ? x / r : 0;
-  const uint16_t* qsrc =
-      static_cast<const uint16_t*>(a.Q) + (t.row0 + row) * a.ldq + (h * r + (x - row * r)) * D + 8 * quad;
-  bf16x8_t q[D / 32];
+  const T* qsrc = static_cast<const T*>(a.Q) + (t.row0 + row) * a.ldq + (h * r + (x - row * r)) * D + E * quad;
+  vec q[QS];
 #pragma unroll
-  for (int s = 0; s < D / 32; ++s) {
-    uint4 u = make_uint4(0, 0, 0, 0);
-    if (live) u = *reinterpret_cast<const uint4*>(qsrc + 32 * s);
-    q[s] = __builtin_bit_cast(bf16x8_t, u);
+  for (int s = 0; s < QS; ++s) {
+    u32x4_t u = {0, 0, 0, 0};
+    if (live) u = *reinterpret_cast<const u32x4_t*>(qsrc + 4 * E * s);
+    q[s] = __builtin_bit_cast(vec, u);
   }
   const int lim = live ? sees(a, t, prefix, row) : 0, lim0 = sees(a, t, prefix, t.x0 / r);
 
@@ -486,58 +510,81 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
   const char* const Kc = static_cast<const char*>(a.k_cache);
   const char* const Vc = static_cast<const char*>(a.v_cache);
   struct Block {
-    u32x4_t k[G::LOADS], v[G::LOADS];
+    u32x4_t k[SH::LOADS], v[SH::LOADS];
   };
   // No load is left out (the waits count them): past the last block all lanes load one place.
   auto load = [&](Block& b, int i) {
     const int64_t at = places.of(a, t.len, h, i);
     const uint32_t mine = i < blocks ? lane * 16 : 0, next = i < blocks ? 1024 : 0;
 #pragma unroll
-    for (int c = 0; c < G::LOADS; ++c) b.k[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(Kc + at + c * next + mine));
+    for (int c = 0; c < SH::LOADS; ++c)
+      b.k[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(Kc + at + c * next + mine));
 #pragma unroll
-    for (int c = 0; c < G::LOADS; ++c) b.v[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(Vc + at + c * next + mine));
+    for (int c = 0; c < SH::LOADS; ++c)
+      b.v[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(Vc + at + c * next + mine));
   };
   f32x4_t o[D / 16];
 #pragma unroll
   for (int e = 0; e < D / 16; ++e) o[e] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   float m = kLowest, l = 0.0f;
   bool unsound = false;
-  const float c2 = a.c2;
-  // LDS addresses: K, then V.  Row LOAD_ROWS c + lr of K has chunk ch at ch ^ kswz of the row,
-  // in which c and lr set bits apart; V^T's read: 16 lanes read four keys x 16 columns, lane
-  // i receives column i of the four keys.
-  const uint32_t K = (uint32_t)(uintptr_t)(lds_t)smem + wave * 2 * SH::BLOCK, V = K + SH::BLOCK;
-  const int lr = lane / G::CHUNKS, ch = lane % G::CHUNKS, vr = (lane >> 2) & 3;
-  const uint32_t kdst = K + lr * G::ROW + ((ch ^ G::kswz(lr)) << 4);
-  const uint32_t ksrc = K + ql * G::ROW + ((quad ^ G::kswz(ql)) << 4);
-  const uint32_t vdst = V + lr * G::ROW + ((ch ^ G::vswz(lr)) << 4);
-  const uint32_t vsrc = V + (4 * quad + vr) * G::ROW + (G::vswz(vr) << 4) + (lane & 3) * 8;
+  const float c2 = a.c2, c2_low = a.c2_low;
+  // LDS addresses: K, then V; a lane writes chunk ch of row lr of each load
   typedef __attribute__((address_space(3))) u32x4_t* l16_t;
+  typedef __attribute__((address_space(3))) float* l4_t;
+  const uint32_t K = (uint32_t)(uintptr_t)(lds_t)smem + wave * 2 * SH::BLOCK, V = K + SH::BLOCK;
+  const int lr = lane / SH::CHUNKS, ch = lane % SH::CHUNKS, vr = (lane >> 2) & 3;
+  uint32_t kdst, ksrc, vdst, vsrc;
+  if constexpr (sizeof(T) == 2) {
+    // Row LOAD_ROWS c + lr of K has chunk ch at ch ^ kswz of the row, in which c and lr set
+    // bits apart.  V^T's read: 16 lanes read four keys x 16 columns, lane i receives
+    // column i of the four keys.
+    using G = Geo<D>;
+    kdst = K + lr * SH::ROW + ((ch ^ G::kswz(lr)) << 4);
+    ksrc = K + ql * SH::ROW + ((quad ^ G::kswz(ql)) << 4);
+    vdst = V + lr * SH::ROW + ((ch ^ G::vswz(lr)) << 4);
+    vsrc = V + (4 * quad + vr) * SH::ROW + (G::vswz(vr) << 4) + (lane & 3) * 8;
+  } else {
+    kdst = K + lr * SH::LDS_ROW + ch * 16;
+    ksrc = K + ql * SH::LDS_ROW + quad * 16;
+    vdst = V + lr * SH::LDS_ROW + ch * 16;
+    vsrc = V + 4 * quad * SH::LDS_ROW + ql * 4;
+  }
   auto use = [&](Block& b, int i) {
     const int kb = first + step * i;
     f32x4_t st = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int c = 0; c < G::LOADS; ++c)
-      *(l16_t)(lds_t)(uintptr_t)((kdst ^ G::kswz(G::LOAD_ROWS * c) << 4) + c * 1024) = b.k[c];
+    for (int c = 0; c < SH::LOADS; ++c) {
+      const uint32_t to = sizeof(T) == 2 ? kdst ^ Geo<D>::kswz(SH::LOAD_ROWS * c) << 4 : kdst;
+      *(l16_t)(lds_t)(uintptr_t)(to + c * SH::LOAD_ROWS * SH::LDS_ROW) = b.k[c];
+    }
 #pragma unroll
-    for (int s = 0; s < D / 32; ++s)
-      st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-          __builtin_bit_cast(bf16x8_t, *(l16_t)(lds_t)(uintptr_t)(ksrc ^ s << 6)), q[s], st, 0, 0, 0);
+    for (int s = 0; s < QS; ++s) {
+      const uint32_t from = sizeof(T) == 2 ? ksrc ^ s << 6 : ksrc + s * 64;
+      const vec k = __builtin_bit_cast(vec, *(l16_t)(lds_t)(uintptr_t)from);
+      if constexpr (sizeof(T) == 2) {
+        st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[s], st, 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) st = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j], q[s][j], st, 0, 0, 0);
+      }
+    }
     if (kb + 16 > lim0) {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         if (kb + 4 * quad + k >= lim) st[k] = -INFINITY;
       // past the end: zeros; keys that some pairs see and others do not: looked at
 #pragma unroll
-      for (int c = 0; c < G::LOADS; ++c)
-        if (kb + G::LOAD_ROWS * c + lr >= k1) b.v[c] = u32x4_t{0, 0, 0, 0};
+      for (int c = 0; c < SH::LOADS; ++c)
+        if (kb + SH::LOAD_ROWS * c + lr >= k1) b.v[c] = u32x4_t{0, 0, 0, 0};
       u16x2_t bits = {0, 0};
 #pragma unroll
-      for (int c = 0; c < G::LOADS; ++c) larger_bits(bits, b.v[c]);
+      for (int c = 0; c < SH::LOADS; ++c) larger_bits<T>(bits, b.v[c]);
       if (min(kb + 16, k1) > lim0) unsound = unsound || __any(bits[0] >= 0x7f80 || bits[1] >= 0x7f80);
     }
 #pragma unroll
-    for (int c = 0; c < G::LOADS; ++c) *(l16_t)(lds_t)(uintptr_t)(vdst + c * 1024) = b.v[c];
+    for (int c = 0; c < SH::LOADS; ++c)
+      *(l16_t)(lds_t)(uintptr_t)(vdst + c * SH::LOAD_ROWS * SH::LDS_ROW) = b.v[c];
     const float bm = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3])) * c2;
     if (__any(bm > m + kRescale)) {
       const float mn = fmaxf(m, quad_max(bm));
@@ -547,18 +594,32 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
 #pragma unroll
       for (int e = 0; e < D / 16; ++e) o[e] *= sc;
     }
-    bf16x4_t pb;
+    float p[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const float p = __builtin_amdgcn_exp2f(fmaf(st[k], c2, -m));
-      l += p;
-      pb[k] = (__bf16)p;
+      float e = fmaf(st[k], c2, -m);
+      // float32: with the rest of scale log2(e), whose rounding would be off by up to 2^-24 of the score
+      if (sizeof(T) == 4 && st[k] > kLowest) e = fmaf(st[k], c2_low, e);
+      p[k] = __builtin_amdgcn_exp2f(e);
+      l += p[k];
     }
+    if constexpr (sizeof(T) == 2) {
+      bf16x4_t pb;
 #pragma unroll
-    for (int e = 0; e < D / 16; ++e) {
-      const bf16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((ltr_t)(lds_t)(uintptr_t)(vsrc ^ e << 5));
-      o[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, v), __builtin_bit_cast(s16x4_t, pb),
-                                                       o[e], 0, 0, 0);
+      for (int k = 0; k < 4; ++k) pb[k] = (__bf16)p[k];
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e) {
+        const bf16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((ltr_t)(lds_t)(uintptr_t)(vsrc ^ e << 5));
+        o[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, v),
+                                                         __builtin_bit_cast(s16x4_t, pb), o[e], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(*(l4_t)(lds_t)(uintptr_t)(vsrc + k * SH::LDS_ROW + e * 64), p[k],
+                                                      o[e], 0, 0, 0);
     }
   };
   if (blocks > 0) {
@@ -575,7 +636,7 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
   }
   l = quad_sum(l);
   if (unsound) {
-    KeyByKey<D, 16> kk;
+    KeyByKey<T, D, 16> kk;
     kk.start(h);
     for (int i = 0; i < blocks; ++i) {
       const int kb = first + step * i;
@@ -587,6 +648,7 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
     for (int e = 0; e < D / 16; ++e) o[e] = kk.o[e];
   }
 
+  typedef T out4_t __attribute__((ext_vector_type(4)));
   const int pre = ceil_div(prefix_tokens(a, g, prefix_len), a.plan.chunk_prefix);
   if (spread) {
     if (!live) return;
@@ -597,10 +659,10 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
 #pragma unroll
     for (int e = 0; e < D / 16; ++e) {
       if (u.done) {
-        bf16x4_t v;
+        out4_t v;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = (__bf16)(o[e][k] * inv);
-        *reinterpret_cast<bf16x4_t*>(static_cast<__bf16*>(a.O) + u.pair * D + 16 * e + 4 * quad) = v;
+        for (int k = 0; k < 4; ++k) v[k] = (T)(o[e][k] * inv);
+        *reinterpret_cast<out4_t*>(static_cast<T*>(a.O) + u.pair * D + 16 * e + 4 * quad) = v;
       } else {
         *reinterpret_cast<f32x4_t*>(u.o + 16 * e + 4 * quad) = o[e];
       }
@@ -620,39 +682,36 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
     ml[(kWaves + wave) * kThin + ql] = l;
   }
   __syncthreads();
-  constexpr int E = D / 16;                           // elements of a thread, sixteen threads to a pair
-  const int c = tid >> 4, e0 = (tid & 15) * E, xc = t.x0 + c;
+  constexpr int F = D / 16;                           // elements of a thread, sixteen threads to a pair
+  const int c = tid >> 4, e0 = (tid & 15) * F, xc = t.x0 + c;
   if (xc >= t.pairs) return;
   const Out u = prefix ? prefix_place(a, t, h, xc, chunk)
                        : own_place(a, t, h, xc, chunk, ceil_div(sees(a, t, false, xc / r), chunk_keys), pre);
   if (u.pair < 0) return;
-  float M = kLowest, L = 0.0f, acc[E];
+  float M = kLowest, L = 0.0f, acc[F];
 #pragma unroll
   for (int v = 0; v < kWaves; ++v) M = fmaxf(M, ml[v * kThin + c]);
 #pragma unroll
-  for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+  for (int e = 0; e < F; ++e) acc[e] = 0.0f;
 #pragma unroll
   for (int v = 0; v < kWaves; ++v) {
     const float f = __builtin_amdgcn_exp2f(ml[v * kThin + c] - M);
     L = fmaf(ml[(kWaves + v) * kThin + c], f, L);
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = fmaf(part[(v * kThin + c) * SH::PART_ROW + e0 + e], f, acc[e]);
+    for (int e = 0; e < F; ++e) acc[e] = fmaf(part[(v * kThin + c) * SH::PART_ROW + e0 + e], f, acc[e]);
   }
   if ((tid & 15) == 0) store_ml(a, u, M, L);
-  if (u.done) {
-    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-    __bf16* dst = static_cast<__bf16*>(a.O) + u.pair * D + e0;
+  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
 #pragma unroll
-    for (int e = 0; e < E; e += 4) {
-      bf16x4_t v;
+  for (int e = 0; e < F; e += 4) {
+    if (u.done) {
+      out4_t v;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = (__bf16)(acc[e + k] * inv);
-      *reinterpret_cast<bf16x4_t*>(dst + e) = v;
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < E; e += 4)
+      for (int k = 0; k < 4; ++k) v[k] = (T)(acc[e + k] * inv);
+      *reinterpret_cast<out4_t*>(static_cast<T*>(a.O) + u.pair * D + e0 + e) = v;
+    } else {
       *reinterpret_cast<float4*>(u.o + e0 + e) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+    }
   }
 }
 
@@ -980,7 +1039,7 @@ __device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool 
   w.l = half_sum(w.l);
   if (unsound) {
     const AttendArgs& f = arguments();
-    KeyByKey<D, 32> kk;
+    KeyByKey<__bf16, D, 32> kk;
     kk.start(h);
     for (int i = 0; i < n; ++i) {
       const bool p = v0 + i < before;
@@ -1025,48 +1084,55 @@ __device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool 
 }
 
 // One launch for all tiles: the prefixes' (thin or tall), the sequences' tall ones, the
-// sequences' thin ones, in this order.
-template <int D>
+// sequences' thin ones, in this order; the last workgroup looks for errors in the batch's
+// entries, wherever they are.  float32 has thin tiles only, several to a longer sequence.
+template <typename T, int D>
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a) {
-  __shared__ __attribute__((aligned(1024))) char smem[kAttendLds];
+  constexpr bool BF16 = sizeof(T) == 2;
+  constexpr int LDS = ThinShape<T, D>::LDS > kAttendLds || !BF16 ? ThinShape<T, D>::LDS : kAttendLds;
+  __shared__ __attribute__((aligned(1024))) char smem[LDS];
   const AttendPlan& p = a.plan;
   const int heads = a.shape.kv_heads;
   int id = blockIdx.x;
-  if (id == 0) {
+  if (id == p.prefix_blocks + p.tall_blocks + p.thin_blocks) {
     report_entries(a, false);
     if (a.prefix.count > 0) report_entries(a, true);
+    return;
   }
   Tile t;
   // block id of `tiles` tiles, the key heads and the chunks
-  const int tall = p.prefix_tall && id < p.prefix_blocks ? 1 : id >= p.prefix_blocks && id < p.prefix_blocks + p.tall_blocks ? 2 : 0;
-  if (tall) {
-    const bool prefix = tall == 1;
-    if (!prefix) id -= p.prefix_blocks;
-    const int tiles = prefix ? p.prefix_tiles : p.tall_tiles;
-    // Workgroup w runs on XCD w % 8: 32 tiles that follow one another, and so mostly share
-    // their keys, on each in turn.
-    if ((id | 255) < (prefix ? p.prefix_blocks : p.tall_blocks)) id = (id & ~255) + (id % 8) * 32 + id / 8 % 32;
-    const int rest = id / tiles, tile = tiles - 1 - (id - rest * tiles);
-    if (!find_tile<kTall>(a, prefix, tile, t)) return;
-    if (!prefix && t.pairs <= kThin) return;                                 // a thin tile's
-    tall_tile<D>(a, smem, prefix, t, rest % heads, rest / heads);
-    return;
+  if constexpr (BF16) {
+    const bool prefix = p.prefix_tall && id < p.prefix_blocks;
+    if (prefix || (id >= p.prefix_blocks && id < p.prefix_blocks + p.tall_blocks)) {
+      if (!prefix) id -= p.prefix_blocks;
+      const int tiles = prefix ? p.prefix_tiles : p.tall_tiles;
+      // Workgroup w runs on XCD w % 8: 32 tiles that follow one another, and so mostly share
+      // their keys, on each in turn.
+      if ((id | 255) < (prefix ? p.prefix_blocks : p.tall_blocks)) id = (id & ~255) + (id % 8) * 32 + id / 8 % 32;
+      const int rest = id / tiles, tile = tiles - 1 - (id - rest * tiles);
+      if (!find_tile<kTall>(a, prefix, tile, t)) return;
+      if (!prefix && t.pairs <= kThin) return;                               // a thin tile's
+      tall_tile<D>(a, smem, prefix, t, rest % heads, rest / heads);
+      return;
+    }
   }
   const bool prefix = id < p.prefix_blocks;
   if (!prefix) id -= p.prefix_blocks + p.tall_blocks;
-  const int tiles = prefix ? p.prefix_tiles : a.runs.count;
   const bool spread = !prefix && p.spread;
+  const int tiles = prefix ? p.prefix_tiles : p.thin_tiles;
   const int per = spread ? heads / kWaves : heads, rest = id / tiles, tile = id - rest * tiles, chunk = rest / per;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int h = spread ? (rest - chunk * per) * kWaves + wave : rest - chunk * per;
-  Places<Geo<D>::ROW> places;
+  const int key = chunk * (prefix ? p.chunk_prefix : p.chunk_thin) + (spread ? 0 : 16 * wave);
+  Places<D * (int)sizeof(T)> places;
   int g = -1;
-  if (prefix) {
-    if (!find_tile<kThin>(a, true, tile, t)) return;
-    places.prime(a, a.prefix, t.seg, chunk * p.chunk_prefix + 16 * wave, kThinStep);
+  if (prefix || p.thin_tiled) {
+    if (!find_tile<kThin>(a, prefix, tile, t)) return;
+    places.prime(a, prefix ? a.prefix : a.runs, t.seg, key, spread ? 16 : kThinStep);
+    if (!prefix) g = group_of(a, t.seg);
   } else {                                           // a sequence to a tile; longer ones are the tall tiles'
     t.seg = tile;
-    places.prime(a, a.runs, t.seg, chunk * p.chunk_thin + (spread ? 0 : 16 * wave), spread ? 16 : kThinStep);
+    places.prime(a, a.runs, t.seg, key, spread ? 16 : kThinStep);
     const int tokens = tokens_of(a.runs, t.seg, t.len), rows = rows_of(a.rows, t.seg, t.row0, t.n);
     g = group_of(a, t.seg);
     const int64_t pairs = (int64_t)t.n * ratio(a);
@@ -1075,174 +1141,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a) {
     t.x0 = 0;
     t.table = a.runs.table + (int64_t)t.seg * a.runs.width;
   }
-  thin_tile<D>(a, smem, prefix, t, places, h, chunk, g, spread);
-}
-
-// ---------------------------------------------------------------- float32
-
-// 16 pairs; each of four waves takes every fourth block of 16 keys (one page),
-// straight from memory into the operands' registers:
-//   S^T = K Q^T (v_mfma_f32_16x16x4_f32): lane l holds key l % 16 and, of each 16
-//   elements of a row, the four from 4 (l / 16) on, one to each of four products;
-//   scores of keys 4 (l / 16) + i of pair l % 16;
-//   O^T += V^T P: lane l holds element l % 16 of each 16 of the keys 4 (l / 16) + i.
-template <int D>
-__global__ __launch_bounds__(64 * kWaves) void attend_f32_kernel(AttendArgs a) {
-  constexpr int PART_ROW = D + 4;
-  __shared__ __attribute__((aligned(16))) float smem[kWaves * kThin * (PART_ROW + 2)];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 15, quad = lane >> 4;
-  int id = blockIdx.x;
-  if (id == 0) {
-    report_entries(a, false);
-    if (a.prefix.count > 0) report_entries(a, true);
-  }
-  const bool prefix = id < a.plan.prefix_blocks;
-  if (!prefix) id -= a.plan.prefix_blocks;
-  const int tiles = prefix ? a.plan.prefix_tiles : a.plan.thin_tiles;
-  const int rest = id / tiles, h = rest % a.shape.kv_heads, chunk = rest / a.shape.kv_heads;
-  Tile t;
-  if (!find_tile<kThin>(a, prefix, id - rest * tiles, t)) return;
-  const int chunk_keys = prefix ? a.plan.chunk_prefix : a.plan.chunk_thin;
-  const int g = prefix ? -1 : group_of(a, t.seg), prefix_len = g < 0 ? 0 : a.prefix.len[g];
-  const int r = ratio(a);
-  const int tile_end = sees(a, t, prefix, (min(t.x0 + kThin, t.pairs) - 1) / r);
-  const int k0 = chunk * chunk_keys;
-  if (k0 >= tile_end && (prefix || chunk > 0)) return;
-  const int k1 = min(tile_end, k0 + chunk_keys);
-
-  const int x = t.x0 + ql;
-  const bool live = x < t.pairs;
-  const int row = live ? x / r : 0;
-  const float* qsrc = static_cast<const float*>(a.Q) + (t.row0 + row) * a.ldq + (h * r + (x - row * r)) * D + 4 * quad;
-  f32x4_t q[D / 16];
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
-    q[s] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    if (live) q[s] = *reinterpret_cast<const f32x4_t*>(qsrc + 16 * s);
-  }
-  const int lim = live ? sees(a, t, prefix, row) : 0;
-  const int lim0 = sees(a, t, prefix, t.x0 / r);
-
-  f32x4_t o[D / 16];
-#pragma unroll
-  for (int e = 0; e < D / 16; ++e) o[e] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-  float m = kLowest, l = 0.0f;
-  const int blocks = k1 - k0 > 16 * wave ? (k1 - k0 - 16 * wave + 16 * kWaves - 1) / (16 * kWaves) : 0;
-  Places<4 * D> places;
-  places.prime(a, prefix ? a.prefix : a.runs, t.seg, k0 + 16 * wave, kThinStep);
-  for (int i = 0; i < blocks; ++i) {
-    const int kb = k0 + 16 * (wave + kWaves * i);
-    const int64_t at = places.of(a, t.len, h, i);
-    const float* K = reinterpret_cast<const float*>(static_cast<const char*>(a.k_cache) + at);
-    const float* V = reinterpret_cast<const float*>(static_cast<const char*>(a.v_cache) + at);
-    const int in = k1 - kb;                          // keys of the block
-    f32x4_t k[D / 16];
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-      k[s] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-      if (ql < in) k[s] = *reinterpret_cast<const f32x4_t*>(K + ql * D + 16 * s + 4 * quad);
-    }
-    float v[D / 16][4];
-#pragma unroll
-    for (int e = 0; e < D / 16; ++e)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        v[e][g] = 0.0f;
-        if (4 * quad + g < in) v[e][g] = V[(4 * quad + g) * D + 16 * e + ql];
-      }
-    f32x4_t st = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) st = __builtin_amdgcn_mfma_f32_16x16x4f32(k[s][g], q[s][g], st, 0, 0, 0);
-    const bool masked = kb + 16 > lim0;
-    if (masked) {
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        if (kb + 4 * quad + g >= lim) st[g] = -INFINITY;
-    }
-    float bm = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3]));
-    bm = fmaxf(bm, __shfl_xor(bm, 16, 64));
-    bm = fmaxf(bm, __shfl_xor(bm, 32, 64));
-    const float mn = fmaxf(m, bm * a.c2);
-    const float sc = exp2f(m - mn);
-    m = mn;
-    l *= sc;
-#pragma unroll
-    for (int e = 0; e < D / 16; ++e) o[e] *= sc;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      st[g] = exp2f(fmaf(st[g], a.c2, -m));
-      l += st[g];
-    }
-    if (masked && min(kb + 16, k1) > lim0) {         // a hidden key's value would be weighed with 0
-      bool bad = false;
-#pragma unroll
-      for (int e = 0; e < D / 16; ++e)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) bad |= !(fabsf(v[e][g]) <= FLT_MAX);
-      if (__any(bad)) {
-        for (int g = 0; g < 4; ++g) {
-          for (int qd = 0; qd < 4; ++qd) {
-            const float p = __shfl(st[0], ql + 16 * qd, 64);
-            const int key = 4 * qd + g;
-            if (kb + key < lim) {
-#pragma unroll
-              for (int e = 0; e < D / 16; ++e)
-                o[e] += p * *reinterpret_cast<const f32x4_t*>(V + key * D + 16 * e + 4 * quad);
-            }
-          }
-          st[0] = st[1];
-          st[1] = st[2];
-          st[2] = st[3];
-        }
-        continue;
-      }
-    }
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-#pragma unroll
-      for (int e = 0; e < D / 16; ++e) o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e][g], st[g], o[e], 0, 0, 0);
-  }
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
-
-  float* ml = smem + kWaves * 16 * PART_ROW;         // part [wave][pair][PART_ROW], then [m, l][wave][pair]
-#pragma unroll
-  for (int e = 0; e < D / 16; ++e)
-    *reinterpret_cast<f32x4_t*>(smem + (wave * 16 + ql) * PART_ROW + 16 * e + 4 * quad) = o[e];
-  if (quad == 0) {
-    ml[wave * 16 + ql] = m;
-    ml[(kWaves + wave) * 16 + ql] = l;
-  }
-  __syncthreads();
-  constexpr int E = D / 16;                          // sixteen threads to a pair
-  const int c = tid >> 4, e0 = (tid & 15) * E;
-  const int xc = t.x0 + c;
-  if (xc >= t.pairs) return;
-  const int pre = ceil_div(prefix_tokens(a, g, prefix_len), a.plan.chunk_prefix);
-  const Out u = prefix ? prefix_place(a, t, h, xc, chunk)
-                       : own_place(a, t, h, xc, chunk, ceil_div(sees(a, t, false, xc / r), chunk_keys), pre);
-  if (u.pair < 0) return;
-  float M = kLowest, L = 0.0f, acc[E];
-#pragma unroll
-  for (int y = 0; y < kWaves; ++y) M = fmaxf(M, ml[y * 16 + c]);
-#pragma unroll
-  for (int e = 0; e < E; ++e) acc[e] = 0.0f;
-#pragma unroll
-  for (int y = 0; y < kWaves; ++y) {
-    const float f = exp2f(ml[y * 16 + c] - M);
-    L = fmaf(ml[(kWaves + y) * 16 + c], f, L);
-#pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = fmaf(smem[(y * 16 + c) * PART_ROW + e0 + e], f, acc[e]);
-  }
-  if ((tid & 15) == 0) store_ml(a, u, M, L);
-  const float inv = !u.done ? 1.0f : L == 0.0f ? 0.0f : 1.0f / L;
-  float* dst = u.done ? static_cast<float*>(a.O) + u.pair * D : u.o;
-#pragma unroll
-  for (int e = 0; e < E; e += 4)
-    *reinterpret_cast<float4*>(dst + e0 + e) =
-        make_float4(acc[e] * inv, acc[e + 1] * inv, acc[e + 2] * inv, acc[e + 3] * inv);
+  thin_tile<T, D>(a, smem, prefix, t, places, h, chunk, g, spread);
 }
 
 // ---------------------------------------------------------------- joining the parts
@@ -1258,11 +1157,13 @@ __global__ __launch_bounds__(64 * kWaves) void combine_kernel(AttendArgs a, int 
   const int Hq = a.shape.q_heads;
   const AttendPlan& p = a.plan;
   int64_t row = -1, base = 0;                        // the row's parts from pair `base` on
+  int2 counts = make_int2(0, 0);
   const int head = (int)(at % Hq);
   if (tall || p.by_row) {
     row = at / Hq;
     base = row * Hq;
     bool live = row < a.rows.rows;
+    if (live) counts = a.row_parts[row];             // (beside the loads that tell whether it is a row)
     if (live && a.rows.padded) {
       const int64_t s = row / a.rows.rows_per_seq;
       live = s < a.runs.count && row - s * a.rows.rows_per_seq < a.rows.info[s] &&
@@ -1284,12 +1185,13 @@ __global__ __launch_bounds__(64 * kWaves) void combine_kernel(AttendArgs a, int 
       if (i < n && (int64_t)n * ratio(a) <= p.short_pairs) {
         row = first + i;
         base = short_base(a, row, (int)s, i);
+        counts = a.row_parts[row];
       }
     }
   }
   int own = 0, pre = 0;
   if (row >= 0) {
-    const int2 c = a.row_parts[row];
+    const int2 c = counts;
     own = c.x;
     pre = c.y;
     // (after an error in the batch's entries a row may have no count)
@@ -1388,16 +1290,17 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
   const int64_t heads = s.kv_heads, S = runs.count, G = prefix.count;
   const bool f32 = s.dtype == SP_F32;
   const bool own_tall = !f32 && longest > kThin;
+  p.thin_tiled = f32 && longest > kThin;
   // float32 has no tall tiles: every sequence is short, and its prefix is shared
   p.short_pairs = (int)(f32 || longest < kFuse ? longest : kFuse);
   if (p.short_pairs < 1) p.short_pairs = 1;
   p.by_row = longest <= p.short_pairs;
   p.short_rows = (int)((p.short_pairs + r - 1) / r);
-  p.thin_tiles = (int)(f32 ? pairs / kThin + S : S);
+  p.thin_tiles = (int)(p.thin_tiled ? pairs / kThin + S : S);
   // a wave to a head where there are enough heads for all waves of the device
-  p.spread = !f32 && heads % kWaves == 0 && S * heads >= 2048;
+  p.spread = heads % kWaves == 0 && S * heads >= 2048;
   const int64_t units = p.spread ? heads / kWaves : heads;
-  p.chunk_thin = chunk_of((f32 ? std::max(S, pairs / kThin) : S) * units, runs.max_len, 256, 2048, kThinStep);
+  p.chunk_thin = chunk_of((p.thin_tiled ? std::max(S, pairs / kThin) : S) * units, runs.max_len, 256, 2048, kThinStep);
   p.thin_blocks = p.thin_tiles * units * (runs.max_len > 0 ? parts_of(runs.max_len, p.chunk_thin) : 1);
   p.short_parts = parts_of(runs.max_len, p.chunk_thin);
   if (own_tall) {
@@ -1437,11 +1340,8 @@ void launch_combine(const AttendArgs& a, int64_t pairs, int parts, int tall, hip
 template <typename T, int D>
 void launch_attend(const AttendArgs& a, hipStream_t stream) {
   const AttendPlan& p = a.plan;
-  const dim3 grid((unsigned)(p.prefix_blocks + p.tall_blocks + p.thin_blocks)), block(64 * kWaves);
-  if constexpr (std::is_same<T, float>::value)
-    hipLaunchKernelGGL(attend_f32_kernel<D>, grid, block, 0, stream, a);
-  else
-    hipLaunchKernelGGL(attend_kernel<D>, grid, block, 0, stream, a);
+  const dim3 grid((unsigned)(p.prefix_blocks + p.tall_blocks + p.thin_blocks + 1)), block(64 * kWaves);
+  hipLaunchKernelGGL((attend_kernel<T, D>), grid, block, 0, stream, a);
   if (p.prefix_parts > 0 || p.short_parts > 1)
     launch_combine<T, D>(a, short_slots(a), p.prefix_parts + p.short_parts, 0, stream);
   if (p.tall_parts > 1 && a.rows.max_rows * (int64_t)(a.shape.q_heads / a.shape.kv_heads) > p.short_pairs)

@@ -220,6 +220,7 @@ struct AttendPlan {
   int by_row;                                       // all are short: their parts lie by row, not by sequence
   int prefix_tall;                                  // the prefixes' tiles are tall ones
   int spread;                                       // thin tiles: a wave to a key head, not four
+  int thin_tiled;                                   // sequences have several thin tiles
   int prefix_tiles, tall_tiles, thin_tiles;         // tiles of a key head
   int64_t prefix_blocks, tall_blocks, thin_blocks;  // workgroups
 };
@@ -231,7 +232,7 @@ struct AttendArgs {
   const int32_t* grp_off;
   const void* Q;
   int64_t ldq;
-  float c2;               // scale log2(e)
+  float c2, c2_low;       // scale log2(e), and the rest of it
   int all;                // every row sees its sequence's whole run
   const void* k_cache;
   const void* v_cache;
