@@ -85,16 +85,22 @@ def test_large_groups(gpu_lib, D, per_group):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_a_wave_to_a_head(gpu_lib, dtype):
-    """So many sequences and key heads that each wave takes a head by itself; lengths from
-    none to several chunks, some rows in groups."""
+@pytest.mark.parametrize("longest", [192, 2200])
+def test_many_heads_and_sequences(gpu_lib, dtype, longest):
+    """So many sequences and key heads that, while runs are short, each wave takes a head by
+    itself; lengths from none to several chunks, some rows in groups."""
     S = 40
     lens = [(37 * s) % 90 for s in range(S)]
-    lens[3], lens[11] = 2200, 300
+    lens[3], lens[11] = longest, 177
     b = Batch([1 + (s % 7 == 0) for s in range(S)], lens, heads=(64, 64), D=64, dtype=dtype, prefix=[50, 333],
               cuts=[2, 20, 31], seed=13)
     b.upload()
     b.check(*b.attend())
+    dirty = Batch([2] * S, [2 + n for n in lens[:3]] + [40] * (S - 3), heads=(64, 64), D=64, dtype=dtype, seed=14)
+    dirty.v_cache[dirty.tables[5][39 // 16], :, 39 % 16] = np.nan          # the last token of one run
+    dirty.upload()
+    o, lse = dirty.attend()
+    assert np.isfinite(o[10]).all() and np.isnan(o[11]).all() and np.isfinite(np.delete(o, 11, 0)).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
