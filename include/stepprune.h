@@ -460,7 +460,7 @@ sp_status stepprune_encode(const sp_dims* dims, const void* X, int64_t T_vis,
  * Rows of the model's q, k and v products are described as the compaction
  * leaves them: packed (seq_info = cu_seqlens [S+1]) or padded (seq_info [S] =
  * row counts, sequence s at row s rows_per_seq).  Rows that belong to no
- * sequence are neither read nor written.  One token per sequence is the same
+ * sequence change nothing and are not written.  One token per sequence is the same
  * with one row each.
  *
  * dtype (SP_BF16, SP_F32) applies to q, k, v, the cache and the output; scores,
@@ -492,8 +492,9 @@ typedef struct {
                                new row of sequence s has slot len[s] - (its rows) */
   int32_t count;            /* S for the sequences, G for the prefixes */
   int32_t table_width;
-  int32_t max_len;          /* upper bound on any len, <= table_width page_size; a longer run is a
-                               device error (SP_DEV_GROUP_TOO_LARGE) and its outputs are undefined */
+  int32_t max_len;          /* upper bound on any len, <= table_width page_size and <= 2^30; a longer
+                               run is a device error (SP_DEV_GROUP_TOO_LARGE) and its outputs are
+                               undefined */
 } sp_cache_runs;
 
 /* Rotation of q and k by position (host struct).  Pair j of a head's first

@@ -134,6 +134,7 @@ sp_status check_cache_runs(const sp_cache_runs* r, const CacheShape& s, bool poi
   if (!r) return SP_EINVAL;
   if (r->count < 0 || r->table_width < 0 || r->max_len < 0) return SP_EINVAL;
   if (r->max_len > (int64_t)r->table_width << s.page_shift) return SP_EINVAL;
+  if (r->max_len > kMaxCacheTokens) return SP_EUNSUPPORTED;
   if (pointers && r->count > 0 && (!r->len || (r->max_len > 0 && !r->table))) return SP_EINVAL;
   o.table = r->table;
   o.len = r->len;

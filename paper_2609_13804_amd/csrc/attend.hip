@@ -508,10 +508,11 @@ constexpr int kAttendLds = 64 * 1024;      // two workgroups to a compute unit
 // holds pair l % 16, scores of keys 4 (l / 16) + i, output elements 16 t + 4 (l / 16) + i.
 //
 // Bound by memory.  Two blocks are in registers or on their way there, K and V in whole
-// 1 KB loads; through LDS they come into the operands' layouts.  They are read once, so
-// they are not kept in the caches: 128 single tokens of 256 to 8192 keys, 28 heads on 4,
-// 204 us (5.3 TB/s), with ordinary loads 225, and three blocks ahead 207; 64 of 8192 keys
-// 178 us (6.0 TB/s).
+// 1 KB loads; through LDS they come into the operands' layouts.  Where they are read once,
+// they are not kept in the caches (STREAM): 128 single tokens of 256 to 8192 keys, 28 heads
+// on 4, 204 us, with ordinary loads 225, and three blocks ahead 207; float32 prompts,
+// whose tiles read the same keys, lose by it: 32 of 200 rows over 1000 keys, 16 heads of
+// 64, 375 us and 333 with ordinary loads.
 template <typename T, int D>
 struct ThinShape {
   static constexpr int ROW = D * (int)sizeof(T), CHUNKS = ROW / 16, LOAD_ROWS = 1024 / ROW, LOADS = 16 / LOAD_ROWS;
@@ -525,7 +526,13 @@ struct ThinShape {
   static constexpr int LDS = BLOCKS > PARTS ? BLOCKS : PARTS;   // the blocks, then the waves' results
 };
 
-template <typename T, int D>
+template <bool STREAM>
+__device__ __forceinline__ u32x4_t fetch(const char* p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
+  else return *reinterpret_cast<const u32x4_t*>(p);
+}
+
+template <typename T, int D, bool STREAM>
 __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool prefix, const Tile& t,
                                           Places<D * (int)sizeof(T)>& places, int h, int chunk, int g, bool spread) {
   using SH = ThinShape<T, D>;
@@ -567,11 +574,9 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
     const int64_t at = places.of(a, t.len, h, i);
     const uint32_t mine = i < blocks ? lane * 16 : 0, next = i < blocks ? 1024 : 0;
 #pragma unroll
-    for (int c = 0; c < SH::LOADS; ++c)
-      b.k[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(Kc + at + c * next + mine));
+    for (int c = 0; c < SH::LOADS; ++c) b.k[c] = fetch<STREAM>(Kc + at + c * next + mine);
 #pragma unroll
-    for (int c = 0; c < SH::LOADS; ++c)
-      b.v[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(Vc + at + c * next + mine));
+    for (int c = 0; c < SH::LOADS; ++c) b.v[c] = fetch<STREAM>(Vc + at + c * next + mine);
   };
   f32x4_t o[D / 16];
 #pragma unroll
@@ -1136,7 +1141,7 @@ __device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool 
 // One launch for all tiles: the prefixes' (thin or tall), the sequences' tall ones, the
 // sequences' thin ones, in this order; the last workgroup looks for errors in the batch's
 // entries, wherever they are.  float32 has thin tiles only, several to a longer sequence.
-template <typename T, int D>
+template <typename T, int D, bool STREAM>
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a) {
   constexpr bool BF16 = sizeof(T) == 2;
   constexpr int LDS = ThinShape<T, D>::LDS > kAttendLds || !BF16 ? ThinShape<T, D>::LDS : kAttendLds;
@@ -1195,7 +1200,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a) {
     t.x0 = 0;
     t.table = a.runs.table + (int64_t)t.seg * a.runs.width;
   }
-  thin_tile<T, D>(a, smem, prefix, t, places, h, chunk, g, spread);
+  thin_tile<T, D, STREAM>(a, smem, prefix, t, places, h, chunk, g, spread);
 }
 
 // ---------------------------------------------------------------- joining the parts
@@ -1345,6 +1350,7 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
   const bool f32 = s.dtype == SP_F32;
   const bool own_tall = !f32 && longest > kThin;
   p.thin_tiled = f32 && longest > kThin;
+  p.reread = p.thin_tiled || (f32 && G > 0 && pairs > kThin * G);
   // float32 has no tall tiles: every sequence is short, and its prefix is shared
   p.short_pairs = (int)(f32 || longest < kFuse ? longest : kFuse);
   if (p.short_pairs < 1) p.short_pairs = 1;
@@ -1398,7 +1404,10 @@ template <typename T, int D>
 void launch_attend(const AttendArgs& a, hipStream_t stream) {
   const AttendPlan& p = a.plan;
   const dim3 grid((unsigned)(p.prefix_blocks + p.tall_blocks + p.thin_blocks + 1)), block(64 * kWaves);
-  hipLaunchKernelGGL((attend_kernel<T, D>), grid, block, 0, stream, a);
+  if (std::is_same<T, float>::value && p.reread)
+    hipLaunchKernelGGL((attend_kernel<float, D, false>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((attend_kernel<T, D, true>), grid, block, 0, stream, a);
   if (p.prefix_parts > 0 || p.short_parts > 1)
     launch_combine<T, D>(a, short_slots(a), p.prefix_parts + p.short_parts, 0, stream);
   if (p.tall_parts > 1 && a.rows.max_rows * (int64_t)(a.shape.q_heads / a.shape.kv_heads) > p.short_pairs)

@@ -168,6 +168,7 @@ hipError_t launch_compact_positions(const PositionsArgs& a, hipStream_t stream);
 // The paged cache (stepprune.h's sp_cache_* structs, checked): cache.hip
 // appends, attend.hip reads.
 constexpr int kMaxCacheHeads = 1024;        // query heads
+constexpr int kMaxCacheTokens = 1 << 30;    // of a run
 constexpr int kMaxCacheRows = (1 << 26) - 1;// rows times query heads of a key head (a wave a row fits a grid)
 struct CacheShape {
   int q_heads, kv_heads, head_dim, dtype;
@@ -221,6 +222,7 @@ struct AttendPlan {
   int prefix_tall;                                  // the prefixes' tiles are tall ones
   int spread;                                       // thin tiles: a wave to a key head, not four
   int thin_tiled;                                   // sequences have several thin tiles
+  int reread;                                       // thin tiles read the same keys
   int prefix_tiles, tall_tiles, thin_tiles;         // tiles of a key head
   int64_t prefix_blocks, tall_blocks, thin_blocks;  // workgroups
 };

@@ -67,7 +67,7 @@ ROWS = [(dict(rows=-1), "EINVAL"), (dict(max_rows=-1), "EINVAL"), (dict(layout=2
         (dict(seq_info=0), "EINVAL"), (dict(layout=0, rows_per_seq=3), "EINVAL"),
         (dict(layout=0, rows_per_seq=-1), "EINVAL"), (dict(rows=1 << 26), "EUNSUPPORTED")]
 RUNS = [(dict(count=-1), "EINVAL"), (dict(max_len=49), "EINVAL"), (dict(max_len=-1), "EINVAL"),
-        (dict(ptr=0), "EINVAL"), (dict(len_ptr=0), "EINVAL"), (dict(width=-1, max_len=0), "EINVAL")]
+        (dict(width=(1 << 26) + 1, max_len=(1 << 30) + 1), "EUNSUPPORTED"), (dict(ptr=0), "EINVAL"), (dict(len_ptr=0), "EINVAL"), (dict(width=-1, max_len=0), "EINVAL")]
 
 
 def _append(sp, dims=None, rows=None, runs=None, **kw):
