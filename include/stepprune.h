@@ -477,7 +477,7 @@ typedef struct {
 
 /* The rows of a batch (host struct). */
 typedef struct {
-  int64_t rows;             /* rows of the arrays; rows (q_heads / kv_heads) < 2^26 */
+  int64_t rows;             /* rows of the arrays; rows (q_heads / kv_heads) <= 2^25 */
   int32_t layout;           /* SP_LAYOUT_PACKED or SP_LAYOUT_PADDED */
   int32_t rows_per_seq;     /* padded: rows of a sequence's slice; packed: ignored */
   const int32_t* seq_info;  /* device: packed [S+1] offsets from 0, padded [S] counts */
@@ -487,10 +487,10 @@ typedef struct {
 /* Runs of the cache (host struct). */
 typedef struct {
   const int32_t* table;     /* device [count, table_width]: the pages of each run; entries past a
-                               run's tokens are not used */
+                               run's tokens are not used (max_len 0: NULL will do) */
   const int32_t* len;       /* device [count]: tokens of each run, new rows included, so the first
                                new row of sequence s has slot len[s] - (its rows) */
-  int32_t count;            /* S for the sequences, G for the prefixes */
+  int32_t count;            /* S for the sequences, G for the prefixes; <= 2^24 */
   int32_t table_width;
   int32_t max_len;          /* upper bound on any len, <= table_width page_size and <= 2^30; a longer
                                run is a device error (SP_DEV_GROUP_TOO_LARGE) and its outputs are
@@ -565,8 +565,9 @@ enum { SP_ATTEND_ALL = 1u };  /* every row sees its sequence's whole run */
  * A row that sees no token (or only scores of -inf) gives o = 0, lse = -inf.
  * Tokens that a row does not see are no part of its sums, whatever their pages
  * hold (infinite or NaN values of tokens that only later rows see change the
- * order of the sums, so their rounding).  A prefix is read once for the rows of all its sequences.  With
- * prefixes and runs of length 0 this is cross attention to the prefixes.
+ * order of the sums, so their rounding).  A prefix is read once for the rows of all
+ * its sequences.  With prefixes and runs of length 0 this is cross attention to the
+ * prefixes.
  *
  *  Q        [rows, q_heads head_dim], row stride ldq; 16-byte aligned
  *  rows, runs   the batch's sequences (runs->count = S)
@@ -582,7 +583,8 @@ enum { SP_ATTEND_ALL = 1u };  /* every row sees its sequence's whole run */
  *  events   [0] before, [1] after the whole call (or NULL)
  * The bounds rows, max_rows and max_len (not the lengths) decide the split of
  * the work, so a captured call stays right while the lengths grow up to them;
- * lengths far below their bounds cost launches that find nothing to do.
+ * lengths far below their bounds cost launches that find nothing to do, and bounds
+ * that would take 2^24 workgroups in a launch are refused (SP_EUNSUPPORTED).
  * Probabilities weight the values rounded to dtype; all sums are float32.
  */
 sp_status stepprune_cache_attend(const sp_cache_dims* dims, const void* Q, int64_t ldq,

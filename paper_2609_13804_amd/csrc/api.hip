@@ -134,12 +134,12 @@ sp_status check_cache_runs(const sp_cache_runs* r, const CacheShape& s, bool poi
   if (!r) return SP_EINVAL;
   if (r->count < 0 || r->table_width < 0 || r->max_len < 0) return SP_EINVAL;
   if (r->max_len > (int64_t)r->table_width << s.page_shift) return SP_EINVAL;
-  if (r->max_len > kMaxCacheTokens) return SP_EUNSUPPORTED;
+  if (r->max_len > kMaxCacheTokens || r->count > kMaxCacheRuns) return SP_EUNSUPPORTED;
   if (pointers && r->count > 0 && (!r->len || (r->max_len > 0 && !r->table))) return SP_EINVAL;
   o.table = r->table;
   o.len = r->len;
   o.count = r->count;
-  o.width = r->table_width;
+  o.width = r->max_len > 0 ? r->table_width : 0;     // (runs of no tokens need no table)
   o.max_len = r->max_len;
   return SP_OK;
 }
@@ -168,8 +168,9 @@ sp_status check_attend(const sp_cache_dims* dims, const sp_cache_rows* rows, con
   if (st == SP_OK) st = check_cache_rows(rows, a.shape, a.runs.count, pointers, a.rows);
   a.prefix = CacheRuns{};
   if (st == SP_OK && prefix) st = check_cache_runs(prefix, a.shape, pointers, a.prefix);
-  if (st == SP_OK) a.plan = plan_cache_attend(a.shape, a.rows, a.runs, a.prefix);
-  return st;
+  if (st != SP_OK) return st;
+  a.plan = plan_cache_attend(a.shape, a.rows, a.runs, a.prefix);
+  return cache_attend_fits(a) ? SP_OK : SP_EUNSUPPORTED;
 }
 
 // Header; parts of every row; the parts' maxima and sums, and their outputs (none where

@@ -116,7 +116,7 @@ __device__ __forceinline__ bool find_tile(const AttendArgs& a, bool prefix, int 
   const int r = ratio(a);
   const int count = prefix ? a.prefix.count : a.runs.count;
   auto start = [&](int i) {
-    const int s = prefix ? min(max(a.grp_off[i], 0), a.runs.count - 1) : i;
+    const int s = prefix ? min(max(a.grp_off[i], 0), a.runs.count) : i;
     return first_row(a.rows, s) * r / TILE + i;
   };
   t.seg = wave_find_last(count, (int64_t)index, start);
@@ -1335,7 +1335,7 @@ inline int chunk_of(int64_t items, int64_t max_len, int least, int more, int ste
   const int64_t even = std::min(ceil64(2048, items), ceil64(max_len, more));
   const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(kMaxParts, std::max(fill, even)));
   const int64_t keys = ceil64(max_len, parts);
-  return (int)std::max<int64_t>(step, ceil64(keys, step) * step);
+  return (int)std::min<int64_t>(kMaxCacheTokens, std::max<int64_t>(step, ceil64(keys, step) * step));
 }
 
 inline int parts_of(int64_t max_len, int chunk) { return (int)((max_len + chunk - 1) / chunk); }
@@ -1390,14 +1390,24 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
 
 namespace {
 
+// A join of many parts takes a workgroup to a (row, head), else a wave.
+constexpr int kManyParts = 16;
+inline int64_t join_blocks(int64_t pairs, int parts) { return parts > kManyParts ? pairs : (pairs + kWaves - 1) / kWaves; }
+
 template <typename T, int D>
 void launch_combine(const AttendArgs& a, int64_t pairs, int parts, int tall, hipStream_t stream) {
-  const dim3 block(64 * kWaves);
-  if (parts > 16)
-    hipLaunchKernelGGL((combine_kernel<T, D, kWaves>), dim3((unsigned)pairs), block, 0, stream, a, tall);
-  else
-    hipLaunchKernelGGL((combine_kernel<T, D, 1>), dim3((unsigned)((pairs + kWaves - 1) / kWaves)), block, 0, stream, a,
-                       tall);
+  const dim3 grid((unsigned)join_blocks(pairs, parts)), block(64 * kWaves);
+  if (parts > kManyParts) hipLaunchKernelGGL((combine_kernel<T, D, kWaves>), grid, block, 0, stream, a, tall);
+  else hipLaunchKernelGGL((combine_kernel<T, D, 1>), grid, block, 0, stream, a, tall);
+}
+
+// The rows of the short sequences are joined, those of the others.  (Without a row in any
+// sequence there is nothing to join.)
+inline bool joins_short(const AttendArgs& a) {
+  return a.rows.max_rows > 0 && (a.plan.prefix_parts > 0 || a.plan.short_parts > 1);
+}
+inline bool joins_tall(const AttendArgs& a) {
+  return a.plan.tall_parts > 1 && a.rows.max_rows * (int64_t)(a.shape.q_heads / a.shape.kv_heads) > a.plan.short_pairs;
 }
 
 template <typename T, int D>
@@ -1408,13 +1418,21 @@ void launch_attend(const AttendArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((attend_kernel<float, D, false>), grid, block, 0, stream, a);
   else
     hipLaunchKernelGGL((attend_kernel<T, D, true>), grid, block, 0, stream, a);
-  if (p.prefix_parts > 0 || p.short_parts > 1)
+  if (joins_short(a))
     launch_combine<T, D>(a, short_slots(a), p.prefix_parts + p.short_parts, 0, stream);
-  if (p.tall_parts > 1 && a.rows.max_rows * (int64_t)(a.shape.q_heads / a.shape.kv_heads) > p.short_pairs)
+  if (joins_tall(a))
     launch_combine<T, D>(a, a.rows.rows * a.shape.q_heads, p.tall_parts, 1, stream);
 }
 
 }  // namespace
+
+bool cache_attend_fits(const AttendArgs& a) {
+  constexpr int64_t most = (1 << 24) - 1;            // workgroups of 256: a launch has fewer than 2^32 threads
+  const AttendPlan& p = a.plan;
+  return p.prefix_blocks + p.tall_blocks + p.thin_blocks < most &&
+         (!joins_short(a) || join_blocks(short_slots(a), p.prefix_parts + p.short_parts) <= most) &&
+         (!joins_tall(a) || join_blocks(a.rows.rows * a.shape.q_heads, p.tall_parts) <= most);
+}
 
 hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t stream) {
   if (a.rows.rows == 0 || a.runs.count == 0) return hipSuccess;

@@ -11,7 +11,7 @@
 // cosines and sines of their pairs, which it keeps for all the heads of its row
 // that it passes over.  Few rows are bound by the chain of loads from a row to its
 // sequence, length, page and angles; the row's own loads go ahead of it.  Stores are
-// streamed past the caches: 54175 rows of 28 + 8 heads of 128 (997 MB) 172 us (5.8
+// streamed past the caches: 54070 rows of 28 + 8 heads of 128 (997 MB) 172 us (5.8
 // TB/s), with ordinary stores 188; 3400 rows 11.7 and 14.7 us.
 #include "sp_internal.h"
 #include "cache_rows.h"

@@ -1,5 +1,5 @@
 // Global -> LDS loads without register staging, shared by the matrix-core
-// kernels (gemm.hip, encode.hip).
+// kernels (gemm.hip, encode.hip, attend.hip).
 #pragma once
 
 #include "sp_internal.h"

@@ -169,7 +169,8 @@ hipError_t launch_compact_positions(const PositionsArgs& a, hipStream_t stream);
 // appends, attend.hip reads.
 constexpr int kMaxCacheHeads = 1024;        // query heads
 constexpr int kMaxCacheTokens = 1 << 30;    // of a run
-constexpr int kMaxCacheRows = (1 << 26) - 1;// rows times query heads of a key head (a wave a row fits a grid)
+constexpr int kMaxCacheRows = 1 << 25;      // rows times query heads of a key head (a wave a row fits a grid)
+constexpr int kMaxCacheRuns = 1 << 24;
 struct CacheShape {
   int q_heads, kv_heads, head_dim, dtype;
   int page_shift;         // log2 of page_size
@@ -257,6 +258,7 @@ AttendPlan plan_cache_attend(const CacheShape& shape, const CacheRows& rows, con
 inline int64_t short_slots(const AttendArgs& a) {
   return (a.plan.by_row ? a.rows.rows : (int64_t)a.runs.count * a.plan.short_rows) * a.shape.q_heads;
 }
+bool cache_attend_fits(const AttendArgs& a);         // every launch's grid is within the device's limit
 hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t stream);
 
 // C = A B^T for bfloat16 A [M, K] and B [N, K] (rows K-contiguous), bfloat16

@@ -65,9 +65,12 @@ DIMS = [(dict(q_heads=0), "EINVAL"), (dict(kv_heads=0), "EINVAL"), (dict(kv_head
         (dict(pages=0), "EINVAL")]
 ROWS = [(dict(rows=-1), "EINVAL"), (dict(max_rows=-1), "EINVAL"), (dict(layout=2), "EINVAL"),
         (dict(seq_info=0), "EINVAL"), (dict(layout=0, rows_per_seq=3), "EINVAL"),
-        (dict(layout=0, rows_per_seq=-1), "EINVAL"), (dict(rows=1 << 26), "EUNSUPPORTED")]
+        (dict(layout=0, rows_per_seq=-1), "EINVAL"), (dict(rows=1 << 26), "EUNSUPPORTED"),
+        (dict(rows=(1 << 23) + 1), "EUNSUPPORTED")]
 RUNS = [(dict(count=-1), "EINVAL"), (dict(max_len=49), "EINVAL"), (dict(max_len=-1), "EINVAL"),
-        (dict(width=(1 << 26) + 1, max_len=(1 << 30) + 1), "EUNSUPPORTED"), (dict(ptr=0), "EINVAL"), (dict(len_ptr=0), "EINVAL"), (dict(width=-1, max_len=0), "EINVAL")]
+        (dict(width=(1 << 26) + 1, max_len=(1 << 30) + 1), "EUNSUPPORTED"),
+        (dict(count=(1 << 24) + 1), "EUNSUPPORTED"), (dict(ptr=0), "EINVAL"), (dict(len_ptr=0), "EINVAL"),
+        (dict(width=-1, max_len=0), "EINVAL")]
 
 
 def _append(sp, dims=None, rows=None, runs=None, **kw):
@@ -143,6 +146,33 @@ def test_workspace_query(sp):
             assert ws(rows=_rows(sp, **kw)) == 0, kw
     assert ws(runs=_runs(sp, max_len=49)) == 0
     assert ws(runs=_runs(sp, ptr=0, len_ptr=0)) == base            # device pointers are not read
+
+
+def test_largest_bounds(sp):
+    """Bounds at their limits: the split stays within its integers, and what no launch holds
+    is refused."""
+    ws = lambda rows, runs, prefix, **kw: sp.stepprune_cache_workspace_bytes(_dims(sp, **kw), rows, runs, prefix)
+    long = lambda n: _runs(sp, count=n, width=1 << 22, max_len=1 << 30)
+    for heads in (1, 8, 1024):
+        kw = dict(q_heads=heads, kv_heads=heads, page_size=256)
+        n = ws(_rows(sp, rows=64, max_rows=64), long(1), long(1), **kw)       # parts of each (row, head)
+        assert 0 < n <= 3 * 64 * heads * 1024 * 130 * 4 + 4096, (heads, n)
+    # many items: one chunk would be prefix and run together, 2^31 keys
+    many = dict(q_heads=1024, kv_heads=1024, page_size=256)
+    n = ws(_rows(sp, rows=64, max_rows=64), long(1), long(1), **many)
+    assert 0 < n < 1 << 36, n
+    # a wave to each (row, head) to join with the prefix
+    big = dict(q_heads=1024, kv_heads=1024, page_size=16, dtype=sp.SP_F32)
+    few = _runs(sp, count=1)
+    assert ws(_rows(sp, rows=1 << 15, max_rows=1 << 15), few, few, **big) > 0
+    assert ws(_rows(sp, rows=1 << 17, max_rows=1 << 17), few, few, **big) == 0
+    assert _attend(sp, dims=_dims(sp, **big), rows=_rows(sp, rows=1 << 17, max_rows=1 << 17), ldq=1 << 17,
+                   prefix=few, grp_off=FAKE) == sp.SP_EUNSUPPORTED
+    # 2^24 and more workgroups for the tokens: with a wave to a head a quarter of the heads each
+    assert ws(_rows(sp, rows=1 << 15, max_rows=1), _runs(sp, count=1 << 15), None, **big) > 0
+    assert ws(_rows(sp, rows=1 << 16, max_rows=1), _runs(sp, count=1 << 16), None, **big) == 0
+    # runs of no tokens need no table
+    assert _attend(sp, runs=_runs(sp, ptr=0, max_len=0)) == sp.SP_EWORKSPACE
 
 
 def test_no_rows_is_no_work(sp):

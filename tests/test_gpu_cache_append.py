@@ -179,6 +179,18 @@ def test_positions(gpu_lib, layout, axes):
     assert sp.stepprune_read_device_error(ws) == 0
     ref = oracle_cache.compact_positions(vis, io, txt, to, kept, layout, per, np.full((axes, rows), -7))
     assert np.array_equal(pos.cpu().numpy(), ref)
+    # captured and replayed, on other positions each time
+    d_vis, out = ints(vis), torch.full((axes, rows), -7, dtype=torch.int32, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        sp.stepprune_compact_positions(d_vis, *args[1:], out, ws, 256)
+    for n in (1, 2, 3):
+        d_vis.copy_(ints(vis + n))
+        g.replay()
+        torch.cuda.synchronize()
+        ref = oracle_cache.compact_positions(vis + n, io, txt, to, kept, layout, per, np.full((axes, rows), -7))
+        assert np.array_equal(out.cpu().numpy(), ref)
+    assert sp.stepprune_read_device_error(ws) == 0
     # what does not fit, and a kept index outside its image, are recorded
     bad = list(args)
     if per:
@@ -192,6 +204,64 @@ def test_positions(gpu_lib, layout, axes):
     bad[7] = ints(idx)
     sp.stepprune_compact_positions(*bad, pos, ws, 256)
     assert sp.stepprune_read_device_error(ws) == sp.SP_DEV_BAD_OFFSETS
+
+
+@pytest.mark.parametrize("layout", ["packed", "padded"])
+def test_tokens_in_a_graph(gpu_lib, layout):
+    """A captured step (append, then attend) replays while the runs grow by a token each
+    time, on other streams' and eager work between the replays."""
+    b = Batch([1] * 5, [3, 16, 40, 129, 15], heads=(4, 2), D=64, page=16, layout=layout, seed=4)
+    b.upload(max_len=b.tables.shape[1] * 16)
+    # pages for the tokens to come: those that no run has
+    steps, free = 4, sorted(set(range(b.pages)) - {int(p) for p in b.tables.ravel() if p >= 0})
+    for s in range(b.S):
+        used = -(-b.lens[s] // 16)
+        if -(-(b.lens[s] + steps) // 16) > used:
+            b.tables[s, used] = free.pop()
+    b.d_tables.copy_(ints(b.tables))
+    Hq, Hk, D = b.Hq, b.Hk, b.D
+    cs = angles(200, D // 2)
+    d_cs = torch.from_numpy(cs).cuda()
+    rot = sp.cache_rotation(d_cs, D)
+    qkv = torch.zeros(b.rows, (Hq + 2 * Hk) * D, dtype=torch.bfloat16, device="cuda")
+    dq, dk, dv = qkv.split([Hq * D, Hk * D, Hk * D], 1)
+    q_out, o = (torch.full((b.rows, Hq * D), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    nbytes = sp.stepprune_cache_workspace_bytes(b.dims, b.c_rows, b.c_runs)
+    ws = torch.zeros(nbytes, dtype=torch.uint8, device="cuda")
+
+    def step():
+        sp.stepprune_cache_append(b.dims, dq, dq.stride(0), dk, dk.stride(0), dv, dv.stride(0), b.c_rows, b.c_runs,
+                                  rot, q_out, b.d_k, b.d_v, ws, nbytes)
+        sp.stepprune_cache_attend(b.dims, q_out, Hq * D, b.c_rows, b.c_runs, None, None, b.scale, 0, b.d_k, b.d_v, o,
+                                  None, ws, nbytes)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    host = lambda t, H: t.double().cpu().numpy().reshape(-1, H, D)
+    for _ in range(steps):
+        b.lens = [n + 1 for n in b.lens]
+        b.d_lens.copy_(ints(b.lens))
+        q, k, v = (b.values((b.rows, H, D)) for H in (Hq, Hk, Hk))
+        qkv.copy_(torch.cat([device(t, "bf16").view(b.rows, -1) for t in (q, k, v)], 1))
+        g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (q_out, o, b.d_k, b.d_v)]
+        ref = oracle_cache.append(b.k_cache, b.v_cache, q, k, v, b.first, b.counts, b.tables, b.lens, cs, None,
+                                  [D // 2])
+        live = b.live()
+        for t, r in zip((host(got[0], Hq)[live], got[2].double().cpu().numpy(), got[3].double().cpu().numpy()),
+                        (ref[0][live], ref[1], ref[2])):
+            assert (np.isnan(t) == np.isnan(r)).all()
+            r = np.nan_to_num(r)
+            assert (np.abs(np.nan_to_num(t) - r) <= 2.0 ** -8 * np.abs(r) * 1.01 + 4 * U32 * 8).all()
+        b.q = host(got[0], Hq)
+        b.k_cache, b.v_cache = got[2].double().cpu().numpy(), got[3].double().cpu().numpy()
+        b.check(host(got[1], Hq), None)
+        step()                                          # the same tokens once more, eagerly
+        torch.cuda.synchronize()
+        for t, e in zip(got, (q_out, o, b.d_k, b.d_v)):
+            assert torch.equal(torch.nan_to_num(t), torch.nan_to_num(e))
+    assert sp.stepprune_read_device_error(ws) == 0
 
 
 @pytest.mark.parametrize("name", ["tiny_bf16", "small_packed_bf16"])

@@ -85,6 +85,57 @@ def test_large_groups(gpu_lib, D, per_group):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("counts", [[1, 9], [3, 1, 11, 2]])
+def test_empty_groups_behind_the_last(gpu_lib, dtype, counts):
+    """Groups without a sequence at the end of the batch, behind a group of several tiles."""
+    S = len(counts)
+    b = Batch(counts, [n + 20 for n in counts], heads=(8, 2), dtype=dtype, prefix=[40, 90, 33, 5, 70],
+              cuts=[0, 0, S - 1, S, S, S], seed=S)
+    b.upload()
+    b.check(*b.attend())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["packed", "padded"])
+@pytest.mark.parametrize("longest", [5, 90])
+def test_more_segments_than_lanes(gpu_lib, dtype, layout, longest):
+    """More than 64 sequences and more than 64 groups, of tokens, short and longer prompts."""
+    S = 150
+    counts = [(5 * s) % 4 for s in range(S)]
+    for s in range(3, S, 9):
+        counts[s] = longest - s % 5
+    cuts = sorted([0, 2, 2] + list(range(4, 146, 2)) + [149])
+    G = len(cuts) - 1
+    b = Batch(counts, [n + (11 * s) % 60 for s, n in enumerate(counts)], heads=(4, 2), D=64, dtype=dtype, layout=layout,
+              prefix=[(29 * g) % 140 for g in range(G)], cuts=cuts, seed=longest)
+    assert G > 64
+    b.upload()
+    b.check(*b.attend())
+    b.check(*b.attend(see_all=True), see_all=True)
+
+
+def test_padded_slices_of_no_rows(gpu_lib):
+    """Padded slices of no row: nothing is written, whatever rows the arrays have."""
+    b = Batch([0, 0], [40, 700], heads=(4, 2), D=64, layout="padded", prefix=[30], cuts=[0, 2], seed=2)
+    b.upload()
+    assert b.per_seq == 0
+    b.rows = 5
+    b.q = np.ones((5, 4, 64))
+    b.c_rows = sp.cache_rows(5, sp.SP_LAYOUT_PADDED, 0, b.d_info, 3)
+    o, lse = b.attend()
+    assert (o == 7.0).all() and (lse == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_runs_without_a_table(gpu_lib, dtype):
+    """Runs of no token: their table may be NULL, whatever its width."""
+    b = Batch([1, 3, 40], [0, 0, 0], heads=(4, 4), D=64, dtype=dtype, prefix=[77, 300], cuts=[0, 1, 3], seed=3)
+    b.upload()
+    b.c_runs.table, b.c_runs.table_width = None, 4
+    b.check(*b.attend())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("longest", [192, 2200])
 def test_many_heads_and_sequences(gpu_lib, dtype, longest):
     """So many sequences and key heads that, while runs are short, each wave takes a head by
@@ -256,3 +307,32 @@ def test_other_stream_and_graph(gpu_lib):
         torch.cuda.synchronize()
         assert torch.equal(got, out)
     assert sp.stepprune_read_device_error(ws) == 0
+
+
+def test_two_streams_at_once(gpu_lib):
+    """Two batches on two streams, each with its own workspace, get what they get alone."""
+    batches = [Batch([1] * 9, [900 + 7 * s for s in range(9)], heads=(8, 2), prefix=[700], cuts=[0, 9], seed=1),
+               Batch([130, 60, 1], [700, 60, 300], heads=(8, 2), seed=2)]
+    calls, alone, outs = [], [], []
+    for b in batches:
+        b.upload()
+        o, lse = b.attend()
+        b.check(o, lse)
+        q = device(b.q, "bf16").view(b.rows, -1)
+        out = torch.full_like(q, 7.0)
+        nbytes = sp.stepprune_cache_workspace_bytes(b.dims, b.c_rows, b.c_runs, b.c_prefix)
+        ws = torch.zeros(nbytes, dtype=torch.uint8, device="cuda")
+        calls.append(lambda b=b, q=q, out=out, ws=ws, nbytes=nbytes: sp.stepprune_cache_attend(
+            b.dims, q, q.shape[1], b.c_rows, b.c_runs, b.c_prefix, b.d_off, b.scale, 0, b.d_k, b.d_v, out, None, ws,
+            nbytes))
+        alone.append(o)
+        outs.append(out)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in batches]
+    for _ in range(8):
+        for call, stream in zip(calls, streams):
+            with torch.cuda.stream(stream):
+                call()
+    torch.cuda.synchronize()
+    for b, o, out in zip(batches, alone, outs):
+        assert np.array_equal(out.double().cpu().numpy().reshape(o.shape)[b.live()], o[b.live()])
