@@ -48,6 +48,7 @@ typedef __attribute__((address_space(3))) char* lds_t;
 constexpr int kThin = 16, kTall = 128;     // pairs of a tile
 constexpr int kFuse = 64;                  // pairs of a sequence past which it takes its prefix by itself
 constexpr int kWaves = 4;
+constexpr int kWide = 8;                   // of a wide workgroup
 constexpr int kMaxParts = 1024;
 constexpr int kThinStep = 16 * kWaves;     // keys that the waves of a thin tile take together
 constexpr int kTallStep = 64;
@@ -513,7 +514,7 @@ constexpr int kAttendLds = 64 * 1024;      // two workgroups to a compute unit
 // on 4, 204 us, with ordinary loads 225, and three blocks ahead 207; float32 prompts,
 // whose tiles read the same keys, lose by it: 32 of 200 rows over 1000 keys, 16 heads of
 // 64, 375 us and 333 with ordinary loads.
-template <typename T, int D>
+template <typename T, int D, int WAVES>
 struct ThinShape {
   static constexpr int ROW = D * (int)sizeof(T), CHUNKS = ROW / 16, LOAD_ROWS = 1024 / ROW, LOADS = 16 / LOAD_ROWS;
   // LDS rows: bfloat16 as in the tall tiles; float32 padded by 16 bytes, so that 16 rows'
@@ -522,7 +523,7 @@ struct ThinShape {
   static constexpr int BLOCK = 16 * LDS_ROW;                    // 16 keys of K or V
   static constexpr int PART_ROW = D + 4;
   static constexpr int DEPTH = 2;
-  static constexpr int BLOCKS = 2 * kWaves * BLOCK, PARTS = kWaves * kThin * (PART_ROW + 2) * 4;
+  static constexpr int BLOCKS = 2 * WAVES * BLOCK, PARTS = WAVES * kThin * (PART_ROW + 2) * 4;
   static constexpr int LDS = BLOCKS > PARTS ? BLOCKS : PARTS;   // the blocks, then the waves' results
 };
 
@@ -532,10 +533,10 @@ __device__ __forceinline__ u32x4_t fetch(const char* p) {
   else return *reinterpret_cast<const u32x4_t*>(p);
 }
 
-template <typename T, int D, bool STREAM>
+template <typename T, int D, bool STREAM, int WAVES>
 __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool prefix, const Tile& t,
                                           Places<D * (int)sizeof(T)>& places, int h, int chunk, int g, bool spread) {
-  using SH = ThinShape<T, D>;
+  using SH = ThinShape<T, D, WAVES>;
   using vec = typename Chunk<T>::vec;
   constexpr int E = Chunk<T>::N, QS = D / (4 * E);               // query vectors of a lane
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -729,30 +730,30 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
   // the waves' results, joined: part [wave][pair][PART_ROW], then [m, l][wave][pair]
   __syncthreads();
   float* part = reinterpret_cast<float*>(smem);
-  float* ml = part + kWaves * kThin * SH::PART_ROW;
+  float* ml = part + WAVES * kThin * SH::PART_ROW;
 #pragma unroll
   for (int e = 0; e < D / 16; ++e)
     *reinterpret_cast<f32x4_t*>(part + (wave * kThin + ql) * SH::PART_ROW + 16 * e + 4 * quad) = o[e];
   if (quad == 0) {
     ml[wave * kThin + ql] = m;
-    ml[(kWaves + wave) * kThin + ql] = l;
+    ml[(WAVES + wave) * kThin + ql] = l;
   }
   __syncthreads();
   constexpr int F = D / 16;                           // elements of a thread, sixteen threads to a pair
   const int c = tid >> 4, e0 = (tid & 15) * F, xc = t.x0 + c;
-  if (xc >= t.pairs) return;
+  if (c >= kThin || xc >= t.pairs) return;
   const Out u = prefix ? prefix_place(a, t, h, xc, chunk)
                        : own_place(a, t, h, xc, chunk, ceil_div(sees(a, t, false, xc / r), chunk_keys), pre);
   if (u.pair < 0) return;
   float M = kLowest, L = 0.0f, acc[F];
 #pragma unroll
-  for (int v = 0; v < kWaves; ++v) M = fmaxf(M, ml[v * kThin + c]);
+  for (int v = 0; v < WAVES; ++v) M = fmaxf(M, ml[v * kThin + c]);
 #pragma unroll
   for (int e = 0; e < F; ++e) acc[e] = 0.0f;
 #pragma unroll
-  for (int v = 0; v < kWaves; ++v) {
+  for (int v = 0; v < WAVES; ++v) {
     const float f = __builtin_amdgcn_exp2f(ml[v * kThin + c] - M);
-    L = fmaf(ml[(kWaves + v) * kThin + c], f, L);
+    L = fmaf(ml[(WAVES + v) * kThin + c], f, L);
 #pragma unroll
     for (int e = 0; e < F; ++e) acc[e] = fmaf(part[(v * kThin + c) * SH::PART_ROW + e0 + e], f, acc[e]);
   }
@@ -1139,13 +1140,26 @@ __device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool 
   }
 }
 
+// Sequence `seg` as one thin tile, and its group.  False: it has no row, or more than 16 pairs.
+__device__ __forceinline__ bool sequence_tile(const AttendArgs& a, int seg, Tile& t, int& g) {
+  t.seg = seg;
+  const int tokens = tokens_of(a.runs, seg, t.len), rows = rows_of(a.rows, seg, t.row0, t.n);
+  g = group_of(a, seg);
+  const int64_t pairs = (int64_t)t.n * ratio(a);
+  if (rows != SP_DEV_OK || tokens != SP_DEV_OK || pairs == 0 || pairs > kThin) return false;
+  t.pairs = (int)pairs;
+  t.x0 = 0;
+  t.table = a.runs.table + (int64_t)seg * a.runs.width;
+  return true;
+}
+
 // One launch for all tiles: the prefixes' (thin or tall), the sequences' tall ones, the
 // sequences' thin ones, in this order; the last workgroup looks for errors in the batch's
 // entries, wherever they are.  float32 has thin tiles only, several to a longer sequence.
 template <typename T, int D, bool STREAM>
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a) {
   constexpr bool BF16 = sizeof(T) == 2;
-  constexpr int LDS = ThinShape<T, D>::LDS > kAttendLds || !BF16 ? ThinShape<T, D>::LDS : kAttendLds;
+  constexpr int LDS = ThinShape<T, D, kWaves>::LDS > kAttendLds || !BF16 ? ThinShape<T, D, kWaves>::LDS : kAttendLds;
   __shared__ __attribute__((aligned(1024))) char smem[LDS];
   const AttendPlan& p = a.plan;
   const int heads = a.shape.kv_heads;
@@ -1191,17 +1205,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a) {
     places.prime(a, prefix ? a.prefix : a.runs, t.seg, key, spread ? 16 : kThinStep);
     if (!prefix) g = group_of(a, t.seg);
   } else {                                           // a sequence to a tile; longer ones are the tall tiles'
-    t.seg = tile;
-    places.prime(a, a.runs, t.seg, key, spread ? 16 : kThinStep);
-    const int tokens = tokens_of(a.runs, t.seg, t.len), rows = rows_of(a.rows, t.seg, t.row0, t.n);
-    g = group_of(a, t.seg);
-    const int64_t pairs = (int64_t)t.n * ratio(a);
-    if (rows != SP_DEV_OK || tokens != SP_DEV_OK || pairs == 0 || pairs > kThin) return;
-    t.pairs = (int)pairs;
-    t.x0 = 0;
-    t.table = a.runs.table + (int64_t)t.seg * a.runs.width;
+    places.prime(a, a.runs, tile, key, spread ? 16 : kThinStep);
+    if (!sequence_tile(a, tile, t, g)) return;
   }
-  thin_tile<T, D, STREAM>(a, smem, prefix, t, places, h, chunk, g, spread);
+  thin_tile<T, D, STREAM, kWaves>(a, smem, prefix, t, places, h, chunk, g, spread);
+}
+
+// Few sequences, of at most 16 pairs and not too many keys: eight waves to a sequence and key
+// head, so that no parts are left for a second launch to join.
+template <int D>
+__global__ __launch_bounds__(64 * kWide, 2) void wide_kernel(AttendArgs a) {
+  __shared__ __attribute__((aligned(1024))) char smem[ThinShape<__bf16, D, kWide>::LDS];
+  if (blockIdx.x == a.plan.thin_blocks) {
+    report_entries(a, false);
+    return;
+  }
+  const int heads = a.shape.kv_heads, seg = blockIdx.x / heads, h = blockIdx.x - seg * heads;
+  Places<2 * D> places;
+  places.prime(a, a.runs, seg, 16 * __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), 16 * kWide);
+  Tile t;
+  int g;
+  if (!sequence_tile(a, seg, t, g)) return;
+  thin_tile<__bf16, D, true, kWide>(a, smem, false, t, places, h, 0, -1, false);
 }
 
 // ---------------------------------------------------------------- joining the parts
@@ -1365,6 +1390,25 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
   p.spread = heads % kWaves == 0 && S * heads >= 2048 && runs.max_len <= 192;
   const int64_t units = p.spread ? heads / kWaves : heads;
   p.chunk_thin = chunk_of((p.thin_tiled ? std::max(S, pairs / kThin) : S) * units, runs.max_len, 256, 2048, kThinStep);
+  // A wide workgroup to a sequence and key head, where those are no more than the compute
+  // units and either the runs are short or nearly all units have one.  us, in chunks (joined by
+  // a second launch from 257 tokens on) / wide, heads of 128, all runs of one length:
+  //    32 of 64, 256, 400, 707, 1024 tokens  5.9 / 5.3, 7.5 / 6.3, 10.1 / 7.4, 10.2 / 9.3, 10.3 / 10.8
+  //   128 of 256, 707, 2048                  7.6 / 6.5, 13.8 / 11.9, 24.9 / 26.4
+  //   256 of 256, 707, 2048                  7.8 / 7.1, 19.9 / 15.9, 44.7 / 40.9
+  //   512 of 256, 707, 2048                  12.8 / 14.6, 30.3 / 31.4, 81.1 / 80.7
+  // float32's products take a compute unit too long: 16 of 640 tokens, heads of 64, 10.4 / 11.5.
+  const int64_t items = S * heads;
+  p.wide = !f32 && !own_tall && prefix.max_len == 0 && items <= 256 &&
+           (runs.max_len <= 768 || (items > 128 && runs.max_len <= 2048));
+  if (p.wide) {
+    p.spread = 0;
+    p.chunk_thin = (runs.max_len / (16 * kWide) + 1) * 16 * kWide;
+    p.chunk_prefix = kTallStep;
+    p.short_parts = 1;
+    p.thin_blocks = items;
+    return p;
+  }
   p.thin_blocks = p.thin_tiles * units * (runs.max_len > 0 ? parts_of(runs.max_len, p.chunk_thin) : 1);
   p.short_parts = parts_of(runs.max_len, p.chunk_thin);
   if (own_tall) {
@@ -1415,7 +1459,8 @@ template <typename T, int D>
 void launch_attend(const AttendArgs& a, hipStream_t stream) {
   const AttendPlan& p = a.plan;
   const dim3 grid((unsigned)(p.prefix_blocks + p.tall_blocks + p.thin_blocks + 1)), block(64 * kWaves);
-  if (std::is_same<T, float>::value && p.reread)
+  if (p.wide) hipLaunchKernelGGL((wide_kernel<D>), grid, dim3(64 * kWide), 0, stream, a);
+  else if (std::is_same<T, float>::value && p.reread)
     hipLaunchKernelGGL((attend_kernel<float, D, false>), grid, block, 0, stream, a);
   else
     hipLaunchKernelGGL((attend_kernel<T, D, true>), grid, block, 0, stream, a);

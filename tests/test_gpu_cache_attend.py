@@ -197,6 +197,33 @@ def test_hidden_tokens_have_no_influence(gpu_lib, dtype, bad, D):
     assert not np.isfinite(od[41:, :2]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("longest", [130, 760, 1900])
+def test_few_short_sequences(gpu_lib, dtype, D, longest):
+    """A few sequences of one to eight rows, runs from none to several blocks a wave, some of
+    less tokens than rows; tokens that only the last row sees are NaN in one of them."""
+    counts, lens = [1, 8, 0, 3, 8, 2, 8], [0, 3, 9, longest, longest - 2, 2, 129]
+    b = Batch(counts, lens, heads=(4, 2), D=D, dtype=dtype, layout="padded", pad=1, seed=D)
+    b.upload()
+    b.check(*b.attend())
+    b.check(*b.attend(see_all=True), see_all=True)
+    clean, _ = b.attend()
+    tol, _ = b.bounds(*b.oracle())
+    b.v_cache[b.tables[4][(lens[4] - 1) // 16], :, (lens[4] - 1) % 16] = np.nan
+    b.upload()
+    o, _ = b.attend()
+    last = b.first[4] + 7
+    assert np.isnan(o[last]).all()
+    rows = np.setdiff1d(b.live(), [last])
+    assert np.isfinite(o[rows]).all() and (np.abs(o[rows] - clean[rows]) <= 2 * tol[rows]).all()
+    none = Batch([1, 2], [0, 0], heads=(4, 2), D=D, dtype=dtype)           # no token at all
+    none.upload()
+    none.c_runs.table = None
+    o, lse = none.attend()
+    assert (o == 0).all() and np.isneginf(lse).all()
+
+
 def test_infinite_scores(gpu_lib):
     """A key that scores -inf weighs nothing, also when it comes first; rows whose every
     score is -inf give zeros."""
