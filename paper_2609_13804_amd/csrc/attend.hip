@@ -95,6 +95,7 @@ struct Tile {
   int n;                  // rows of the segment
   int len;                // tokens of its run
   const int32_t* table;   // its pages
+  int group, before;      // (tall tiles of a sequence) its group, -1 without one, and the tokens of the prefix
 };
 
 __device__ __forceinline__ int ratio(const AttendArgs& a) { return a.shape.q_heads / a.shape.kv_heads; }
@@ -139,16 +140,35 @@ __device__ __forceinline__ bool find_tile(const AttendArgs& a, bool prefix, int 
   return tokens_of(runs, t.seg, t.len) == SP_DEV_OK;
 }
 
+// The group of sequence s: -1 without one.
+__device__ __forceinline__ int group_of(const AttendArgs& a, int s) {
+  if (a.prefix.count == 0) return -1;
+  const int g = wave_find_last(a.prefix.count, s, [&](int i) { return a.grp_off[i]; });
+  return s < a.grp_off[g] || s >= a.grp_off[g + 1] ? -1 : g;
+}
+
+// The tokens of its prefix.  (`len` is the prefixes' entry: loaded ahead of its use)
+__device__ __forceinline__ int prefix_tokens(const AttendArgs& a, int g, int len) {
+  return g < 0 || len < 0 || len > a.prefix.max_len ? 0 : len;
+}
+
+__device__ __forceinline__ void find_prefix(const AttendArgs& a, Tile& t) {
+  t.group = group_of(a, t.seg);
+  t.before = prefix_tokens(a, t.group, t.group < 0 ? 0 : a.prefix.len[t.group]);
+}
+
 // The same for tall tiles of up to 64 segments, a lane to each: the segments with the most
 // keys come first, and of a segment the tiles with the most, so that the launch ends with
 // small work.  (64 prompts on prefixes of 894 to 2264 tokens, 28 heads on 4: in the order
 // of the batch 200 us, in this one 175.)
 constexpr int kSorted = 64;
-__device__ __forceinline__ bool find_sorted_tile(const AttendArgs& a, bool prefix, int index, Tile& t) {
-  const int lane = threadIdx.x & 63, r = ratio(a);
+// LDS: kSorted entries of `table`, the wave's own.
+__device__ __forceinline__ bool find_sorted_tile(const AttendArgs& a, bool prefix, int index, Tile& t, uint2* table) {
+  const int lane = threadIdx.x & 63, r = ratio(a), G = a.prefix.count;
   const CacheRuns& runs = prefix ? a.prefix : a.runs;
+  const bool grouped = !prefix && G > 0 && G <= 64;          // a lane to a group
   int64_t row0 = 0, n = 0;
-  int len = 0, keys = 0, tiles = 0;
+  int len = 0, tiles = 0, off = INT_MAX, end = 0, tokens = 0, group = -1;
   if (lane < runs.count) {
     int rows = 0;
     bool ok;
@@ -159,24 +179,36 @@ __device__ __forceinline__ bool find_sorted_tile(const AttendArgs& a, bool prefi
       n = rows;
     }
     ok = tokens_of(runs, lane, len) == SP_DEV_OK && ok;
-    keys = len;
-    if (!prefix && a.prefix.count > 0 && n * r > kFuse) {
-      int g = 0;                                     // the last group that begins at or before the sequence
-      for (int hi = a.prefix.count; hi - g > 1;) {
-        const int mid = (g + hi) >> 1;
-        if (a.grp_off[mid] <= lane) g = mid;
-        else hi = mid;
-      }
-      if (a.grp_off[g] <= lane && lane < a.grp_off[g + 1])
-        keys = (int)min((int64_t)INT_MAX, (int64_t)keys + max(0, a.prefix.len[g]));
-    }
     if (ok) tiles = (int)((n * r + kTall - 1) / kTall);
   }
-  int start = 0;
-  for (int k = 0; k < runs.count; ++k) {
-    const int other = __builtin_amdgcn_readlane(keys, k), size = __builtin_amdgcn_readlane(tiles, k);
-    if (other > keys || (other == keys && k < lane)) start += size;
+  if (grouped) {
+    if (lane < G) {
+      off = a.grp_off[lane];
+      end = a.grp_off[lane + 1];
+      tokens = a.prefix.len[lane];
+    }
+    int* const offsets = reinterpret_cast<int*>(table);
+    offsets[lane] = off;
+    for (int k = 0; k < G; k += 8)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) group += offsets[k + i] <= lane;
+    end = __shfl(end, max(group, 0));
+    tokens = __shfl(tokens, max(group, 0));
+    if (lane >= end) group = -1;
+    tokens = prefix_tokens(a, group, tokens);
   }
+  // order: keys, then the place in the batch
+  const uint32_t keys = (uint32_t)len + (grouped && n * r > kFuse ? (uint32_t)tokens : 0);
+  const uint32_t order = min(keys, (1u << 26) - 1) << 6 | (63 - lane);
+  table[lane] = make_uint2(order, (uint32_t)tiles);
+  int start = 0;
+#pragma unroll 1
+  for (int k = 0; k < runs.count; k += 16)           // (the lanes past the last segment have no tiles)
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const uint4 v = *reinterpret_cast<const uint4*>(table + k + i);
+      start += (v.x > order ? v.y : 0) + (v.z > order ? v.w : 0);
+    }
   const uint64_t mine = __ballot(index >= start && index < start + tiles);
   if (mine == 0) return false;
   t.seg = __builtin_ctzll(mine);
@@ -186,6 +218,9 @@ __device__ __forceinline__ bool find_sorted_tile(const AttendArgs& a, bool prefi
   t.pairs = t.n * r;
   t.x0 = (__builtin_amdgcn_readlane(start, t.seg) + __builtin_amdgcn_readlane(tiles, t.seg) - 1 - index) * kTall;
   t.table = runs.table + (int64_t)t.seg * runs.width;
+  t.group = __builtin_amdgcn_readlane(group, t.seg);
+  t.before = __builtin_amdgcn_readlane(tokens, t.seg);
+  if (!prefix && G > 64) find_prefix(a, t);
   return true;
 }
 
@@ -206,18 +241,6 @@ __device__ __forceinline__ int sees(const AttendArgs& a, const Tile& t, bool pre
   if (prefix || a.all) return t.len;
   const int64_t v = (int64_t)t.len - t.n + row + 1;
   return v < 0 ? 0 : (int)v;
-}
-
-// The group of sequence s: -1 without one.
-__device__ __forceinline__ int group_of(const AttendArgs& a, int s) {
-  if (a.prefix.count == 0) return -1;
-  const int g = wave_find_last(a.prefix.count, s, [&](int i) { return a.grp_off[i]; });
-  return s < a.grp_off[g] || s >= a.grp_off[g + 1] ? -1 : g;
-}
-
-// The tokens of its prefix.  (`len` is the prefixes' entry: loaded ahead of its use)
-__device__ __forceinline__ int prefix_tokens(const AttendArgs& a, int g, int len) {
-  return g < 0 || len < 0 || len > a.prefix.max_len ? 0 : len;
 }
 
 __device__ __forceinline__ const int32_t* pages_of(const AttendArgs& a, bool prefix, int i) {
@@ -421,52 +444,27 @@ __device__ __forceinline__ void clear_rows(char* rows, int from) {
     if (c + lane >= from * Geo<D>::CHUNKS) *reinterpret_cast<uint4*>(rows + (c + lane) * 16) = make_uint4(0, 0, 0, 0);
 }
 
-// The larger magnitudes by the bits of their upper halves (bfloat16: of both halves of
-// four bytes); infinite and NaN from 0x7f80 on.
-template <typename T>
-__device__ __forceinline__ void larger_bits(u16x2_t& m, u32x4_t v) {
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2_t, v[k] & (sizeof(T) == 2 ? 0x7fff7fffu : 0x7fff0000u)));
-}
-
-// Whether the values of tokens from .. to - 1 of a run, which some of the workgroup's pairs
-// see and others do not, hold one: at most as many tokens as the tile has rows.
-template <int D>
-__device__ __forceinline__ bool hidden_unsound(const AttendArgs& a, const int32_t* table, int h, int from, int to) {
-  if (from >= to) return false;
-  u16x2_t m = {0, 0};
-  for (int c = threadIdx.x; c < (to - from) * Geo<D>::CHUNKS; c += 64 * kWaves) {
-    const int key = from + c / Geo<D>::CHUNKS;
-    const int64_t at = place_of<Geo<D>::ROW>(a, checked_page(a, table[key >> a.shape.page_shift]), h, key);
-    larger_bits<__bf16>(m, *reinterpret_cast<const u32x4_t*>(static_cast<const char*>(a.v_cache) + at +
-                                                             c % Geo<D>::CHUNKS * 16));
-  }
-  return __syncthreads_or(m[0] >= 0x7f80 || m[1] >= 0x7f80);
-}
-
 // In a tile, a key that some pairs see and others do not is weighed with 0 for those,
-// which is NaN where its value is infinite or NaN.  A wave that meets one begins again
-// here, key by key, each pair over the keys that it sees alone (a hundred times slower,
-// and never needed by sound data).  Lane l holds pair l % PAIRS; with p = l / PAIRS of P
-// lanes a pair and E elements in 16 bytes, elements E (P s + p) + 0 .. E - 1 of its query
-// in q[s] and 4 (P g + p) + 0 .. 3 of its output in o[g].
-template <typename T, int D, int PAIRS>
+// which is NaN where its value is infinite or NaN.  A wave with such a key whose outputs are
+// not all finite begins again here, key by key, each pair over the keys that it sees alone
+// (a hundred times slower, and never needed by sound data).  Lane l holds pair l % PAIRS;
+// with p = l / PAIRS of P lanes a pair and E elements in 16 bytes, elements E (P s + p) + 0
+// .. E - 1 of its query in q[s] and 4 (P g + p) + 0 .. 3 of its output in elements 4 g + 0
+// .. 3 of o, whose vectors have W.
+template <typename T, int D, int PAIRS, int W, typename O>
 struct KeyByKey {
   using vec = typename Chunk<T>::vec;
   typedef T vec4 __attribute__((ext_vector_type(4)));
   static constexpr int P = 64 / PAIRS, E = Chunk<T>::N;
-  f32x4_t o[D / (4 * P)];
-  float m, l;
-  int head;
-  __device__ __forceinline__ void start(int h) {
+  O& o;
+  float &m, &l;
+  __device__ __forceinline__ KeyByKey(O& out, float& max, float& sum) : o(out), m(max), l(sum) {
 #pragma unroll
-    for (int g = 0; g < D / (4 * P); ++g) o[g] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int e = 0; e < D / P; ++e) o[e / W][e % W] = 0.0f;
     m = kLowest;
     l = 0.0f;
-    head = h;
   }
-  __device__ __forceinline__ void add(const AttendArgs& a, const int32_t* table, const vec (&q)[D / (E * P)],
+  __device__ __forceinline__ void add(const AttendArgs& a, const int32_t* table, int head, const vec (&q)[D / (E * P)],
                                       int from, int to, int lim) {
     const int p = (threadIdx.x & 63) / PAIRS;
 #pragma unroll 1
@@ -492,7 +490,10 @@ struct KeyByKey {
         for (int g = 0; g < D / (4 * P); ++g) {
           const vec4 v = *reinterpret_cast<const vec4*>(V + sizeof(vec4) * (P * g + p));
 #pragma unroll
-          for (int k = 0; k < 4; ++k) o[g][k] = fmaf(wt, (float)v[k], o[g][k] * f);
+          for (int k = 0; k < 4; ++k) {
+            const int e = 4 * g + k;
+            o[e / W][e % W] = fmaf(wt, (float)v[k], o[e / W][e % W] * f);
+          }
         }
       }
     }
@@ -583,7 +584,6 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
 #pragma unroll
   for (int e = 0; e < D / 16; ++e) o[e] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   float m = kLowest, l = 0.0f;
-  bool unsound = false;
   const float c2 = a.c2, c2_low = a.c2_low;
   // LDS addresses: K, then V; a lane writes chunk ch of row lr of each load
   typedef __attribute__((address_space(3))) u32x4_t* l16_t;
@@ -629,14 +629,10 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         if (kb + 4 * quad + k >= lim) st[k] = -INFINITY;
-      // past the end: zeros; keys that some pairs see and others do not: looked at
+      // past the end: zeros
 #pragma unroll
       for (int c = 0; c < SH::LOADS; ++c)
         if (kb + SH::LOAD_ROWS * c + lr >= k1) b.v[c] = u32x4_t{0, 0, 0, 0};
-      u16x2_t bits = {0, 0};
-#pragma unroll
-      for (int c = 0; c < SH::LOADS; ++c) larger_bits<T>(bits, b.v[c]);
-      if (min(kb + 16, k1) > lim0) unsound = unsound || __any(bits[0] >= 0x7f80 || bits[1] >= 0x7f80);
     }
 #pragma unroll
     for (int c = 0; c < SH::LOADS; ++c)
@@ -692,17 +688,19 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
     }
   }
   l = quad_sum(l);
-  if (unsound) {
-    KeyByKey<T, D, 16> kk;
-    kk.start(h);
+  float finite = 0.0f;                               // NaN: no
+  if (lim0 < k1) {                                   // some pairs do not see all keys
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) finite = fmaf(o[e][k], 0.0f, finite);
+  }
+  if (__any(finite != 0.0f)) {
+    KeyByKey<T, D, 16, 4, decltype(o)> kk(o, m, l);
     for (int i = 0; i < blocks; ++i) {
       const int kb = first + step * i;
-      kk.add(a, t.table, q, kb, min(kb + 16, k1), lim);
+      kk.add(a, t.table, h, q, kb, min(kb + 16, k1), lim);
     }
-    m = kk.m;
-    l = kk.l;
-#pragma unroll
-    for (int e = 0; e < D / 16; ++e) o[e] = kk.o[e];
   }
 
   typedef T out4_t __attribute__((ext_vector_type(4)));
@@ -950,12 +948,9 @@ __device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool 
   const int ql = lane & 31, half = lane >> 5, r = ratio(a);
   int g = -1, pre = 0, P = 0;                        // parts of the prefix apart; its tokens taken here
   if (!prefix) {
-    g = group_of(a, t.seg);
-    P = prefix_tokens(a, g, g < 0 ? 0 : a.prefix.len[g]);
-    if (t.pairs <= kFuse) {
-      pre = ceil_div(P, a.plan.chunk_prefix);
-      P = 0;
-    }
+    g = t.group;
+    if (t.pairs > kFuse) P = t.before;
+    else pre = ceil_div(t.before, a.plan.chunk_prefix);
   }
   const int before = ceil_div(P, kTallStep);
   const int chunk_steps = (prefix ? a.plan.chunk_prefix : a.plan.chunk_tall) / kTallStep;
@@ -1037,7 +1032,6 @@ __device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool 
     if (i == ragged) hide(st, P % kTallStep);
     else hide(st, lim - (v0 + i - before) * kTallStep);
   };
-  bool unsound = false;
   if (n > 0) {
     int64_t at = place(0);
 #pragma unroll
@@ -1047,8 +1041,6 @@ __device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool 
     at = place(1);
 #pragma unroll
     for (int k = 0; k < G::LOADS; ++k) ld.keys(Kc + at, mine + STEP, k);
-    unsound = hidden_unsound<D>(a, t.table, h, max(sees(a, t, prefix, t.x0 / r), (v0 - before) * kTallStep),
-                                min(end, (v0 + n - before) * kTallStep));
     f32x16_t st[2];
     wait_vmcnt<0>();
     __syncthreads();
@@ -1094,49 +1086,64 @@ __device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool 
     if (!idle) pipeline_step<D, false>(w, st, 0, vl + ((n - 1) & 1) * STEP, c2, [](int) {});
   }
   w.l = half_sum(w.l);
-  if (unsound) {
+  float finite = 0.0f;                               // NaN: no
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) finite = fmaf(w.o[e][i], 0.0f, finite);
+  // (some pairs do not see all keys)
+  if (__any(finite != 0.0f) && __any(live && lim < min(end, (v0 + n - before) * kTallStep))) {
     const AttendArgs& f = arguments();
-    KeyByKey<__bf16, D, 32> kk;
-    kk.start(h);
+    KeyByKey<__bf16, D, 32, 16, decltype(w.o)> kk(w.o, w.m, w.l);
     for (int i = 0; i < n; ++i) {
       const bool p = v0 + i < before;
       const int kb = (p ? v0 + i : v0 + i - before) * kTallStep;
-      kk.add(f, pages_of(f, prefix || p, p ? g : t.seg), w.q, kb, min(kb + kTallStep, p ? P : end),
+      kk.add(f, pages_of(f, prefix || p, p ? g : t.seg), h, w.q, kb, min(kb + kTallStep, p ? P : end),
              p ? P : lim);
     }
-    w.m = kk.m;
-    w.l = kk.l;
-#pragma unroll
-    for (int e = 0; e < D / 8; ++e)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) w.o[e >> 2][4 * (e & 3) + k] = kk.o[e][k];
   }
 
-  if (!live) return;
   const AttendArgs& e = arguments();
-  const int row_steps = before + ceil_div(lim, kTallStep);
-  const Out u = prefix ? prefix_place(e, t, h, x, chunk) : own_place(e, t, h, x, chunk, ceil_div(row_steps, chunk_steps), pre);
-  if (u.pair < 0) return;
-  if (half == 0) store_ml(e, u, w.m, w.l);
-  if (u.done) {
-    const float inv = w.l == 0.0f ? 0.0f : 1.0f / w.l;
-    __bf16* dst = static_cast<__bf16*>(e.O) + u.pair * D + 4 * half;
-#pragma unroll
-    for (int b = 0; b < D / 32; ++b)
-#pragma unroll
-      for (int g4 = 0; g4 < 4; ++g4) {
-        bf16x4_t v;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = (__bf16)(w.o[b][4 * g4 + k] * inv);
-        *reinterpret_cast<bf16x4_t*>(dst + 32 * b + 8 * g4) = v;
-      }
-  } else {
+  Out u;
+  u.pair = -1;
+  u.done = false;
+  if (live) {
+    const int row_steps = before + ceil_div(lim, kTallStep);
+    u = prefix ? prefix_place(e, t, h, x, chunk) : own_place(e, t, h, x, chunk, ceil_div(row_steps, chunk_steps), pre);
+  }
+  const bool done = u.pair >= 0 && u.done;
+  if (u.pair >= 0 && half == 0) store_ml(e, u, w.m, w.l);
+  if (u.pair >= 0 && !u.done) {
 #pragma unroll
     for (int b = 0; b < D / 32; ++b)
 #pragma unroll
       for (int g4 = 0; g4 < 4; ++g4)
         *reinterpret_cast<float4*>(u.o + 32 * b + 8 * g4 + 4 * half) =
             make_float4(w.o[b][4 * g4], w.o[b][4 * g4 + 1], w.o[b][4 * g4 + 2], w.o[b][4 * g4 + 3]);
+  }
+  // Rows that are done go through LDS, whose every wave is past the last step's values, so
+  // that they are stored in whole chunks of whole rows.
+  __syncthreads();
+  if (!__any(done)) return;
+  constexpr int OUT = G::ROW + 16;
+  char* const rows = smem + wave * 32 * OUT;
+  const float inv = w.l == 0.0f ? 0.0f : 1.0f / w.l;
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int g4 = 0; g4 < 4; ++g4) {
+      bf16x4_t v;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = (__bf16)(w.o[b][4 * g4 + k] * inv);
+      *reinterpret_cast<bf16x4_t*>(rows + ql * OUT + (32 * b + 8 * g4 + 4 * half) * 2) = v;
+    }
+  const int64_t pair = done ? u.pair : -1;
+#pragma unroll
+  for (int c = 0; c < 32; c += G::LOAD_ROWS) {
+    const int j = c + lane / G::CHUNKS, chunk16 = lane % G::CHUNKS;
+    const int64_t to = (int64_t)((uint64_t)(uint32_t)__shfl((int)(pair >> 32), j) << 32 | (uint32_t)__shfl((int)pair, j));
+    const uint4 v = *reinterpret_cast<const uint4*>(rows + j * OUT + chunk16 * 16);
+    if (to >= 0) *reinterpret_cast<uint4*>(static_cast<char*>(e.O) + to * G::ROW + chunk16 * 16) = v;
   }
 }
 
@@ -1181,10 +1188,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a) {
       // end of the launch, not of each head.
       const int rest = id / heads, h = id - rest * heads, chunk = rest / tiles, tile = rest - chunk * tiles;
       if ((prefix ? a.prefix.count : a.runs.count) <= kSorted) {
-        if (!find_sorted_tile(a, prefix, tile, t)) return;
+        // (the last quarter of the tall tiles' LDS: not written before their first barrier)
+        uint2* const table = reinterpret_cast<uint2*>(smem + 6 * kTallStep * D) + kSorted * ((int)threadIdx.x >> 6);
+        if (!find_sorted_tile(a, prefix, tile, t, table)) return;
       } else {
         if (!find_tile<kTall>(a, prefix, tiles - 1 - tile, t)) return;
         if (!prefix && t.pairs <= kThin) return;                             // a thin tile's
+        if (!prefix) find_prefix(a, t);
       }
       tall_tile<D>(a, smem, prefix, t, h, chunk);
       return;
@@ -1349,7 +1359,7 @@ __global__ __launch_bounds__(64 * kWaves) void combine_kernel(AttendArgs a, int 
 }
 
 // Keys of a chunk, in whole steps, for `items` tiles and key heads: chunks of at least
-// `least` keys until the device's 512 places for workgroups have one each, then of at
+// `least` keys while the device's 512 places for workgroups hold them all, then of at
 // least `more` keys until there are four for each, which evens out unequal lengths.
 // (us: one run of 131001 tokens, 4 key heads, in 512 parts of 256 / 128 of 1024 64 / 56;
 // 128 ragged runs of up to 8192 tokens, 4 key heads, in chunks of 8192 / 2048 / 1024
@@ -1357,7 +1367,7 @@ __global__ __launch_bounds__(64 * kWaves) void combine_kernel(AttendArgs a, int 
 inline int chunk_of(int64_t items, int64_t max_len, int least, int more, int step) {
   auto ceil64 = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
   if (items < 1) items = 1;
-  const int64_t fill = std::min(ceil64(512, items), ceil64(max_len, least));
+  const int64_t fill = std::min(512 / items, ceil64(max_len, least));
   const int64_t even = std::min(ceil64(2048, items), ceil64(max_len, more));
   const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(kMaxParts, std::max(fill, even)));
   const int64_t keys = ceil64(max_len, parts);
