@@ -500,8 +500,6 @@ struct KeyByKey {
   }
 };
 
-constexpr int kAttendLds = 64 * 1024;      // two workgroups to a compute unit
-
 // ---------------------------------------------------------------- the thin tiles
 
 // 16 pairs.  The keys of one head go to all four waves, each every fourth block of 16, and
@@ -1164,9 +1162,10 @@ __device__ __forceinline__ bool sequence_tile(const AttendArgs& a, int seg, Tile
 // sequences' thin ones, in this order; the last workgroup looks for errors in the batch's
 // entries, wherever they are.  float32 has thin tiles only, several to a longer sequence.
 template <typename T, int D, bool STREAM>
-__global__ __launch_bounds__(64 * kWaves, 2) void attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 && D == 64 ? 3 : 2) void attend_kernel(AttendArgs a) {
   constexpr bool BF16 = sizeof(T) == 2;
-  constexpr int LDS = ThinShape<T, D, kWaves>::LDS > kAttendLds || !BF16 ? ThinShape<T, D, kWaves>::LDS : kAttendLds;
+  // the tall tiles' two steps of K and of V: two workgroups to a compute unit, or (D 64) three
+  constexpr int TALL = BF16 ? 8 * kTallStep * D : 0, THIN = ThinShape<T, D, kWaves>::LDS, LDS = TALL > THIN ? TALL : THIN;
   __shared__ __attribute__((aligned(1024))) char smem[LDS];
   const AttendPlan& p = a.plan;
   const int heads = a.shape.kv_heads;
