@@ -1120,7 +1120,8 @@ __device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool 
             make_float4(w.o[b][4 * g4], w.o[b][4 * g4 + 1], w.o[b][4 * g4 + 2], w.o[b][4 * g4 + 3]);
   }
   // Rows that are done go through LDS, whose every wave is past the last step's values, so
-  // that they are stored in whole chunks of whole rows.
+  // that they are stored in whole chunks of whole rows, streamed past the caches (16 prompts
+  // of 256 rows, 28 heads on 4: 29.0 us, kept in the caches 30.3).
   __syncthreads();
   if (!__any(done)) return;
   constexpr int OUT = G::ROW + 16;
@@ -1140,8 +1141,9 @@ __device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool 
   for (int c = 0; c < 32; c += G::LOAD_ROWS) {
     const int j = c + lane / G::CHUNKS, chunk16 = lane % G::CHUNKS;
     const int64_t to = (int64_t)((uint64_t)(uint32_t)__shfl((int)(pair >> 32), j) << 32 | (uint32_t)__shfl((int)pair, j));
-    const uint4 v = *reinterpret_cast<const uint4*>(rows + j * OUT + chunk16 * 16);
-    if (to >= 0) *reinterpret_cast<uint4*>(static_cast<char*>(e.O) + to * G::ROW + chunk16 * 16) = v;
+    const u32x4_t v = *reinterpret_cast<const u32x4_t*>(rows + j * OUT + chunk16 * 16);
+    if (to >= 0)
+      __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t*>(static_cast<char*>(e.O) + to * G::ROW + chunk16 * 16));
   }
 }
 
