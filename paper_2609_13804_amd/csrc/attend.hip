@@ -1243,13 +1243,15 @@ __global__ __launch_bounds__(64 * kWide, 2) void wide_kernel(AttendArgs a) {
 // ---------------------------------------------------------------- joining the parts
 
 // SPLIT waves to a (row, head): each joins every SPLIT-th part, and they join through LDS.
-// Pairs of the short sequences, or (tall) of the rows of the others.
+// The first `short_blocks` workgroups take the pairs of the short sequences, the others (tall)
+// those of the rows of the others.
 template <typename T, int D, int SPLIT>
-__global__ __launch_bounds__(64 * kWaves) void combine_kernel(AttendArgs a, int tall) {
+__global__ __launch_bounds__(64 * kWaves) void combine_kernel(AttendArgs a, int short_blocks) {
   constexpr int E = D / 64, AHEAD = 8;
   __shared__ float red[kWaves][D + 2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, share = wave % SPLIT;
-  const int64_t at = (int64_t)blockIdx.x * (kWaves / SPLIT) + wave / SPLIT;
+  const bool tall = (int)blockIdx.x >= short_blocks;
+  const int64_t at = (int64_t)((int)blockIdx.x - (tall ? short_blocks : 0)) * (kWaves / SPLIT) + wave / SPLIT;
   const int Hq = a.shape.q_heads;
   const AttendPlan& p = a.plan;
   int64_t row = -1, base = 0;                        // the row's parts from pair `base` on
@@ -1375,6 +1377,24 @@ inline int chunk_of(int64_t items, int64_t max_len, int least, int more, int ste
   return (int)std::min<int64_t>(kMaxCacheTokens, std::max<int64_t>(step, ceil64(keys, step) * step));
 }
 
+// The same for tall tiles, whose parts are many rows' outputs to write and to join: parts are
+// doubled while the places hold them and it pays by what was measured.  us: a step alone on
+// its compute unit 0.78 (heads of 64) to 0.97 (128), a join 5 and its bytes at 2.5 TB/s.  (16
+// rows of 64 heads on 8 over 512 / 1024 / 2048 tokens, heads of 64, in 1, 2, 4, 8 parts: 8
+// sequences 15 20 22 27 / 21 23 25 28 / 35 29 28 27; 32 sequences 20 38 45 58 / 26 43 51 63 /
+// 39 52 63 75.)  `joined`: the rows are joined in any case.
+inline int tall_chunk_of(int64_t items, int64_t keys, int64_t pairs, int D, bool joined) {
+  const int64_t steps = std::max<int64_t>(1, (keys + kTallStep - 1) / kTallStep);
+  const auto cost = [&](int64_t parts) {
+    return (double)((steps + parts - 1) / parts) * (0.6 + 0.003 * D) +
+           (parts > 1 || joined ? 5.0 + (double)parts * (double)pairs * D * 8.0 / 2.5e6 : 0.0);
+  };
+  int64_t best = 1;
+  for (int64_t n = 2; n <= steps && n * items <= 512; n *= 2)
+    if (cost(n) < cost(best)) best = n;
+  return (int)std::min<int64_t>(kMaxCacheTokens, (steps + best - 1) / best * kTallStep);
+}
+
 inline int parts_of(int64_t max_len, int chunk) { return (int)((max_len + chunk - 1) / chunk); }
 
 }  // namespace
@@ -1394,11 +1414,12 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
   p.by_row = longest <= p.short_pairs;
   p.short_rows = (int)((p.short_pairs + r - 1) / r);
   p.thin_tiles = (int)(p.thin_tiled ? pairs / kThin + S : S);
-  // A wave to a head, where there are heads enough for all waves of the device and the runs
-  // are short: fewer workgroups to begin and end, less even work.  us, four waves / one to a
-  // head, 128 runs, 32 key heads: 64 tokens 47 / 26, 128 58 / 44, 256 84 / 86, up to 512
-  // 84 / 91.
-  p.spread = heads % kWaves == 0 && S * heads >= 2048 && runs.max_len <= 192;
+  // A wave to a head, where there are heads enough to fill the device and the runs are short:
+  // fewer workgroups to begin and end, less even work.  us, four waves / one to a head, runs of 5,
+  // 64, 128, 192, 256 tokens, heads of 128: 576 runs and key heads 9.6 / 6.1, 9.9 / 7.6,
+  // 11.6 / 10.2, 14.2 / 12.9, 15.9 / 15.5; 1120: 13.6 / 7.0, 15.0 / 10.2, 18.3 / 16.8, 22.7 / 24.1,
+  // 26.4 / 30.8; 1920: 19.2 / 7.2, 22.5 / 11.8, 28.2 / 20.6, 35.3 / 29.4, 41.6 / 38.4.
+  p.spread = heads % kWaves == 0 && S * heads >= 512 && runs.max_len <= 192;
   const int64_t units = p.spread ? heads / kWaves : heads;
   p.chunk_thin = chunk_of((p.thin_tiled ? std::max(S, pairs / kThin) : S) * units, runs.max_len, 256, 2048, kThinStep);
   // A wide workgroup to a sequence and key head, where those are no more than the compute
@@ -1425,7 +1446,7 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
   if (own_tall) {
     const int64_t keys = (prefix.max_len + kTallStep - 1) / kTallStep * kTallStep + (int64_t)runs.max_len;
     p.tall_tiles = (int)(pairs / kTall + S);
-    p.chunk_tall = chunk_of(std::max(S, pairs / kTall) * heads, keys, 512, INT_MAX, kTallStep);
+    p.chunk_tall = tall_chunk_of(std::max(S, pairs / kTall) * heads, keys, pairs * heads, s.head_dim, false);
     p.tall_parts = parts_of(keys, p.chunk_tall);
     p.tall_blocks = p.tall_tiles * heads * (p.tall_parts > 0 ? p.tall_parts : 1);
     if (p.tall_parts > p.short_parts) p.short_parts = p.tall_parts;
@@ -1434,7 +1455,7 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
     p.prefix_tall = !f32 && pairs > kThin * G;
     p.prefix_tiles = (int)(pairs / (p.prefix_tall ? kTall : kThin) + G);
     p.chunk_prefix = p.prefix_tall
-                         ? chunk_of(std::max(G, pairs / kTall) * heads, prefix.max_len, 512, INT_MAX, kTallStep)
+                         ? tall_chunk_of(std::max(G, pairs / kTall) * heads, prefix.max_len, pairs * heads, s.head_dim, true)
                          : chunk_of(std::max(G, pairs / kThin) * heads, prefix.max_len, 256, 2048, kThinStep);
     p.prefix_parts = parts_of(prefix.max_len, p.chunk_prefix);
     p.prefix_blocks = p.prefix_tiles * heads * p.prefix_parts;
@@ -1446,17 +1467,6 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
 
 namespace {
 
-// A join of many parts takes a workgroup to a (row, head), else a wave.
-constexpr int kManyParts = 16;
-inline int64_t join_blocks(int64_t pairs, int parts) { return parts > kManyParts ? pairs : (pairs + kWaves - 1) / kWaves; }
-
-template <typename T, int D>
-void launch_combine(const AttendArgs& a, int64_t pairs, int parts, int tall, hipStream_t stream) {
-  const dim3 grid((unsigned)join_blocks(pairs, parts)), block(64 * kWaves);
-  if (parts > kManyParts) hipLaunchKernelGGL((combine_kernel<T, D, kWaves>), grid, block, 0, stream, a, tall);
-  else hipLaunchKernelGGL((combine_kernel<T, D, 1>), grid, block, 0, stream, a, tall);
-}
-
 // The rows of the short sequences are joined, those of the others.  (Without a row in any
 // sequence there is nothing to join.)
 inline bool joins_short(const AttendArgs& a) {
@@ -1464,6 +1474,19 @@ inline bool joins_short(const AttendArgs& a) {
 }
 inline bool joins_tall(const AttendArgs& a) {
   return a.plan.tall_parts > 1 && a.rows.max_rows * (int64_t)(a.shape.q_heads / a.shape.kv_heads) > a.plan.short_pairs;
+}
+
+// A join of many parts takes a workgroup to a (row, head), else a wave.
+inline bool many_parts(const AttendArgs& a) {
+  const AttendPlan& p = a.plan;
+  return (joins_short(a) && p.prefix_parts + p.short_parts > 16) || (joins_tall(a) && p.tall_parts > 16);
+}
+inline int64_t join_blocks(const AttendArgs& a, int64_t pairs) {
+  return many_parts(a) ? pairs : (pairs + kWaves - 1) / kWaves;
+}
+inline int64_t short_join_blocks(const AttendArgs& a) { return joins_short(a) ? join_blocks(a, short_slots(a)) : 0; }
+inline int64_t tall_join_blocks(const AttendArgs& a) {
+  return joins_tall(a) ? join_blocks(a, a.rows.rows * a.shape.q_heads) : 0;
 }
 
 template <typename T, int D>
@@ -1475,10 +1498,11 @@ void launch_attend(const AttendArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((attend_kernel<float, D, false>), grid, block, 0, stream, a);
   else
     hipLaunchKernelGGL((attend_kernel<T, D, true>), grid, block, 0, stream, a);
-  if (joins_short(a))
-    launch_combine<T, D>(a, short_slots(a), p.prefix_parts + p.short_parts, 0, stream);
-  if (joins_tall(a))
-    launch_combine<T, D>(a, a.rows.rows * a.shape.q_heads, p.tall_parts, 1, stream);
+  const int64_t first = short_join_blocks(a), second = tall_join_blocks(a);
+  if (first + second == 0) return;
+  const dim3 joins((unsigned)(first + second));
+  if (many_parts(a)) hipLaunchKernelGGL((combine_kernel<T, D, kWaves>), joins, block, 0, stream, a, (int)first);
+  else hipLaunchKernelGGL((combine_kernel<T, D, 1>), joins, block, 0, stream, a, (int)first);
 }
 
 }  // namespace
@@ -1487,8 +1511,7 @@ bool cache_attend_fits(const AttendArgs& a) {
   constexpr int64_t most = (1 << 24) - 1;            // workgroups of 256: a launch has fewer than 2^32 threads
   const AttendPlan& p = a.plan;
   return p.prefix_blocks + p.tall_blocks + p.thin_blocks < most &&
-         (!joins_short(a) || join_blocks(short_slots(a), p.prefix_parts + p.short_parts) <= most) &&
-         (!joins_tall(a) || join_blocks(a.rows.rows * a.shape.q_heads, p.tall_parts) <= most);
+         short_join_blocks(a) + tall_join_blocks(a) <= most;
 }
 
 hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t stream) {

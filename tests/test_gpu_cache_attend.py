@@ -173,6 +173,19 @@ def test_long_run_in_parts(gpu_lib):
     b.check(*b.attend())
 
 
+@pytest.mark.parametrize("layout", ["packed", "padded"])
+@pytest.mark.parametrize("longest", [1300, 6001])
+@pytest.mark.parametrize("prefix", [(), (700, 90)])
+def test_prompts_and_tokens_in_parts(gpu_lib, layout, longest, prefix):
+    """A few rows over long runs beside single tokens: the parts of both kinds of sequences,
+    few and many of them, joined in one launch."""
+    counts, lens = [40, 1, 3, 17, 0], [longest, longest - 7, 70, 500, 9]
+    b = Batch(counts, lens, heads=(4, 1), D=64, page=32, layout=layout, prefix=prefix,
+              cuts=[0, 2, 4] if prefix else (), seed=longest)
+    b.upload()
+    b.check(*b.attend())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
 @pytest.mark.parametrize("D", [64, 128])
