@@ -17,7 +17,8 @@
 //   o = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p,  M = max_p m_p.
 //
 // A sequence's pairs to a key head decide what its rows run in:
-//   up to 16          thin tiles (memory-bound: the waves split the keys)
+//   up to 16          thin tiles (memory-bound: the waves split the keys); in a batch of
+//                     few and short ones wide_kernel's, with twice the waves and no parts
 //   more              tall tiles (the waves split the pairs)
 //   more than kFuse   tall tiles that take the prefix's keys first and then its own:
 //                     such a sequence fills tiles by itself, so sharing the prefix's
@@ -160,7 +161,7 @@ __device__ __forceinline__ void find_prefix(const AttendArgs& a, Tile& t) {
 // The same for tall tiles of up to 64 segments, a lane to each: the segments with the most
 // keys come first, and of a segment the tiles with the most, so that the launch ends with
 // small work.  (64 prompts on prefixes of 894 to 2264 tokens, 28 heads on 4: in the order
-// of the batch 200 us, in this one 175.)
+// of the batch 154 us, in this one 137.)
 constexpr int kSorted = 64;
 // LDS: kSorted entries of `table`, the wave's own.
 __device__ __forceinline__ bool find_sorted_tile(const AttendArgs& a, bool prefix, int index, Tile& t, uint2* table) {
@@ -510,9 +511,10 @@ struct KeyByKey {
 // Bound by memory.  Two blocks are in registers or on their way there, K and V in whole
 // 1 KB loads; through LDS they come into the operands' layouts.  Where they are read once,
 // they are not kept in the caches (STREAM): 128 single tokens of 256 to 8192 keys, 28 heads
-// on 4, 204 us, with ordinary loads 225, and three blocks ahead 207; float32 prompts,
-// whose tiles read the same keys, lose by it: 32 of 200 rows over 1000 keys, 16 heads of
-// 64, 375 us and 333 with ordinary loads.
+// on 4, 192 us (5.6 TB/s), with ordinary loads 202, and three blocks ahead 195; float32
+// prompts, whose tiles read the same keys, lose by it: 32 of 200 rows over 1000 keys, 16
+// heads of 64, 375 us and 333 with ordinary loads.  Key heads are innermost here too: 128
+// tokens of 32 heads on 8 prefixes 133 us, with heads outermost 175.
 template <typename T, int D, int WAVES>
 struct ThinShape {
   static constexpr int ROW = D * (int)sizeof(T), CHUNKS = ROW / 16, LOAD_ROWS = 1024 / ROW, LOADS = 16 / LOAD_ROWS;
@@ -875,9 +877,14 @@ __device__ __forceinline__ void weigh(Pairs<D>& w, const f32x16_t (&st)[2], bf16
 // cores and the vector units work at the same time only where their instructions
 // alternate, and a product waits for its operand's LDS read unless that was issued
 // well before; so the order is written down: operands four products ahead, and between
-// the products the step's loads (issue) and the 16 pairs of scores, 10 of them beside the next scores, 6 beside the
-// values of the first 32 keys.  (In the compiler's order 1.17 ms for 8 prompts of 3840
-// rows, 28 heads of 128 on 4.)
+// the products the step's loads (issue) and the 16 pairs of scores, 10 of them beside
+// the next scores, 6 beside the values of the first 32 keys.  pin() keeps the compiler
+// from gathering a kind's work in one place (without it 850 us, with it 841, for 8
+// prompts of 3840 rows, 28 heads of 128 on 4: 1005 TFLOP/s).
+//
+// What bounds it is power: on zeros the same call takes a fifth less time, at 2.4 GHz
+// instead of about 1.8.  Sums of two weights to an instruction, other priorities of waves,
+// operands three or five ahead and other shares of the scores all measured the same.
 template <int D, bool NEXT, typename Issue>
 __device__ __forceinline__ float pipeline_step(Pairs<D>& w, f32x16_t (&st)[2], uint32_t K, uint32_t V, float c2,
                                                Issue issue) {
@@ -892,7 +899,6 @@ __device__ __forceinline__ float pipeline_step(Pairs<D>& w, f32x16_t (&st)[2], u
     for (int n = 0; n < 2; ++n)
 #pragma unroll
       for (int i = 0; i < 16; ++i) nx[n][i] = 0.0f;
-    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       nx[k & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k % AHEAD], w.q[k >> 1], nx[k & 1], 0, 0, 0);
@@ -901,14 +907,12 @@ __device__ __forceinline__ float pipeline_step(Pairs<D>& w, f32x16_t (&st)[2], u
       issue(k);
 #pragma unroll
       for (int e = k * BESIDE / N; e < (k + 1) * BESIDE / N; ++e) weigh(w, st, pb, e, c2);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+      }
   } else {
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) vf[k] = value_operand<D>(V, k);
 #pragma unroll
     for (int e = 0; e < 8; ++e) weigh(w, st, pb, e, c2);
-    __builtin_amdgcn_sched_barrier(0);
   }
   constexpr int DONE = NEXT ? BESIDE : 8;
   float bm = kLowest;
@@ -925,7 +929,6 @@ __device__ __forceinline__ float pipeline_step(Pairs<D>& w, f32x16_t (&st)[2], u
         bm = fmaxf(fmaxf(bm, nx[e >> 4][e & 15]), nx[e >> 4][(e & 15) + 1]);
       pin(bm);
     }
-    __builtin_amdgcn_sched_barrier(0);
   }
   if constexpr (NEXT) {
     st[0] = nx[0];
@@ -1186,7 +1189,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 && D == 64 ? 3 : 2) voi
       const int tiles = prefix ? p.prefix_tiles : p.tall_tiles;
       // Key heads innermost: workgroup w runs on XCD w % 8, so (4, 8, 16, .. key heads) an
       // XCD's L2 holds the keys of one or two heads at a time, and work ends small at the
-      // end of the launch, not of each head.
+      // end of the launch, not of each head (8 prompts of 3840 rows 844 us, heads outermost 874).
       const int rest = id / heads, h = id - rest * heads, chunk = rest / tiles, tile = rest - chunk * tiles;
       if ((prefix ? a.prefix.count : a.runs.count) <= kSorted) {
         // (the last quarter of the tall tiles' LDS: not written before their first barrier)
@@ -1364,9 +1367,9 @@ __global__ __launch_bounds__(64 * kWaves) void combine_kernel(AttendArgs a, int 
 // Keys of a chunk, in whole steps, for `items` tiles and key heads: chunks of at least
 // `least` keys while the device's 512 places for workgroups hold them all, then of at
 // least `more` keys until there are four for each, which evens out unequal lengths.
-// (us: one run of 131001 tokens, 4 key heads, in 512 parts of 256 / 128 of 1024 64 / 56;
+// (us: one run of 131001 tokens, 4 key heads, in 512 parts of 256 / 128 of 1024 68 / 51;
 // 128 ragged runs of up to 8192 tokens, 4 key heads, in chunks of 8192 / 2048 / 1024
-// 229 / 218 / 229: every workgroup costs a few us to begin and to end.)
+// 216 / 192 / 192: every workgroup costs a few us to begin and to end.)
 inline int chunk_of(int64_t items, int64_t max_len, int least, int more, int step) {
   auto ceil64 = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
   if (items < 1) items = 1;
