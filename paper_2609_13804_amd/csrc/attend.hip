@@ -1364,20 +1364,22 @@ __global__ __launch_bounds__(64 * kWaves) void combine_kernel(AttendArgs a, int 
   if (a.lse && lane == 0) a.lse[out] = lse_of(M, L);
 }
 
-// Keys of a chunk, in whole steps, for `items` tiles and key heads: chunks of at least
-// `least` keys while the device's 512 places for workgroups hold them all, then of at
-// least `more` keys until there are four for each, which evens out unequal lengths.
-// (us: one run of 131001 tokens, 4 key heads, in 512 parts of 256 / 128 of 1024 68 / 51;
-// 128 ragged runs of up to 8192 tokens, 4 key heads, in chunks of 8192 / 2048 / 1024
-// 216 / 192 / 192: every workgroup costs a few us to begin and to end.)
-inline int chunk_of(int64_t items, int64_t max_len, int least, int more, int step) {
+// Keys of a thin tile's chunk, in whole steps, for `items` tiles and key heads: runs of more
+// than 256 keys in chunks of at least 256 (few short ones 128) while the device's 512 places for
+// workgroups hold them all, then of at least 2048 until there are four for each, which evens
+// out unequal lengths.  (us: one token of 32 key heads over 707, caches cold, in chunks of 512 /
+// 256 / 128 11.5 / 10.5 / 9.8, 12 ragged ones of 4 over up to 900 13.9 / 12.2 / 12.9; one run of
+// 131001, 4 key heads, in 512 parts of 256 / 128 of 1024 68 / 51; 128 ragged runs of up to 8192,
+// 4 key heads, in chunks of 8192 / 2048 / 1024 216 / 192 / 192: every workgroup costs a few us
+// to begin and to end.)  `alone`: no other parts are joined to these.
+inline int thin_chunk_of(int64_t items, int64_t max_len, bool alone) {
   auto ceil64 = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
   if (items < 1) items = 1;
-  const int64_t fill = std::min(512 / items, ceil64(max_len, least));
-  const int64_t even = std::min(ceil64(2048, items), ceil64(max_len, more));
+  const int64_t fill = max_len <= 256 ? 1 : std::min(512 / items, ceil64(max_len, alone && items <= 32 && max_len <= 1024 ? 128 : 256));
+  const int64_t even = std::min(ceil64(2048, items), ceil64(max_len, 2048));
   const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(kMaxParts, std::max(fill, even)));
   const int64_t keys = ceil64(max_len, parts);
-  return (int)std::min<int64_t>(kMaxCacheTokens, std::max<int64_t>(step, ceil64(keys, step) * step));
+  return (int)std::min<int64_t>(kMaxCacheTokens, std::max<int64_t>(1, ceil64(keys, kThinStep)) * kThinStep);
 }
 
 // The same for tall tiles, whose parts are many rows' outputs to write and to join: parts are
@@ -1424,18 +1426,19 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
   // 26.4 / 30.8; 1920: 19.2 / 7.2, 22.5 / 11.8, 28.2 / 20.6, 35.3 / 29.4, 41.6 / 38.4.
   p.spread = heads % kWaves == 0 && S * heads >= 512 && runs.max_len <= 192;
   const int64_t units = p.spread ? heads / kWaves : heads;
-  p.chunk_thin = chunk_of((p.thin_tiled ? std::max(S, pairs / kThin) : S) * units, runs.max_len, 256, 2048, kThinStep);
+  p.chunk_thin = thin_chunk_of((p.thin_tiled ? std::max(S, pairs / kThin) : S) * units, runs.max_len, prefix.max_len == 0);
   // A wide workgroup to a sequence and key head, where those are no more than the compute
-  // units and either the runs are short or nearly all units have one.  us, in chunks (joined by
-  // a second launch from 257 tokens on) / wide, heads of 128, all runs of one length:
-  //    32 of 64, 256, 400, 707, 1024 tokens  5.9 / 5.3, 7.5 / 6.3, 10.1 / 7.4, 10.2 / 9.3, 10.3 / 10.8
-  //   128 of 256, 707, 2048                  7.6 / 6.5, 13.8 / 11.9, 24.9 / 26.4
-  //   256 of 256, 707, 2048                  7.8 / 7.1, 19.9 / 15.9, 44.7 / 40.9
-  //   512 of 256, 707, 2048                  12.8 / 14.6, 30.3 / 31.4, 81.1 / 80.7
+  // units and the runs are the shorter the fewer they are.  us, caches cold, in chunks (joined by a
+  // second launch from 257 tokens on) / wide, heads of 128, all runs of one length:
+  //    32 of 64, 256, 400, 707 tokens  5.8 / 5.5, 7.5 / 7.4, 10.1 / 8.9, 10.5 / 11.8
+  //    64 of 64, 256, 707              6.0 / 5.7, 7.9 / 7.6, 12.6 / 12.9
+  //   128 of 64, 256, 707, 2048        6.2 / 5.8, 8.1 / 7.9, 16.7 / 14.3, 31.0 / 31.2
+  //   256 of 64, 256, 707, 2048        6.7 / 6.3, 10.3 / 9.9, 23.1 / 19.8, 53.7 / 49.2
+  //   512 of 64, 256, 707              8.5 / 9.9, 15.7 / 17.5, 35.3 / 36.4
   // float32's products take a compute unit too long: 16 of 640 tokens, heads of 64, 10.4 / 11.5.
   const int64_t items = S * heads;
   p.wide = !f32 && !own_tall && prefix.max_len == 0 && items <= 256 &&
-           (runs.max_len <= 768 || (items > 128 && runs.max_len <= 2048));
+           runs.max_len <= (items <= 64 ? 512 : items <= 192 ? 768 : 2048);
   if (p.wide) {
     p.spread = 0;
     p.chunk_thin = (runs.max_len / (16 * kWide) + 1) * 16 * kWide;
@@ -1459,7 +1462,7 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
     p.prefix_tiles = (int)(pairs / (p.prefix_tall ? kTall : kThin) + G);
     p.chunk_prefix = p.prefix_tall
                          ? tall_chunk_of(std::max(G, pairs / kTall) * heads, prefix.max_len, pairs * heads, s.head_dim, true)
-                         : chunk_of(std::max(G, pairs / kThin) * heads, prefix.max_len, 256, 2048, kThinStep);
+                         : thin_chunk_of(std::max(G, pairs / kThin) * heads, prefix.max_len, false);
     p.prefix_parts = parts_of(prefix.max_len, p.chunk_prefix);
     p.prefix_blocks = p.prefix_tiles * heads * p.prefix_parts;
   } else {
