@@ -66,6 +66,10 @@ __device__ __forceinline__ const AttendArgs& arguments() {
   return *(const AttendArgs*)p;
 }
 
+// LDS that lanes of one wave exchange: its accesses are in order by themselves, the
+// compiler's are by this.
+__device__ __forceinline__ void lds_exchanged() { asm volatile("" ::: "memory"); }
+
 // 16 bytes of a type.
 template <typename T>
 struct Chunk;
@@ -190,9 +194,11 @@ __device__ __forceinline__ bool find_sorted_tile(const AttendArgs& a, bool prefi
     }
     int* const offsets = reinterpret_cast<int*>(table);
     offsets[lane] = off;
+    lds_exchanged();
     for (int k = 0; k < G; k += 8)
 #pragma unroll
       for (int i = 0; i < 8; ++i) group += offsets[k + i] <= lane;
+    lds_exchanged();
     end = __shfl(end, max(group, 0));
     tokens = __shfl(tokens, max(group, 0));
     if (lane >= end) group = -1;
@@ -202,6 +208,7 @@ __device__ __forceinline__ bool find_sorted_tile(const AttendArgs& a, bool prefi
   const uint32_t keys = (uint32_t)len + (grouped && n * r > kFuse ? (uint32_t)tokens : 0);
   const uint32_t order = min(keys, (1u << 26) - 1) << 6 | (63 - lane);
   table[lane] = make_uint2(order, (uint32_t)tiles);
+  lds_exchanged();
   int start = 0;
 #pragma unroll 1
   for (int k = 0; k < runs.count; k += 16)           // (the lanes past the last segment have no tiles)
@@ -1139,6 +1146,7 @@ __device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool 
       for (int k = 0; k < 4; ++k) v[k] = (__bf16)(w.o[b][4 * g4 + k] * inv);
       *reinterpret_cast<bf16x4_t*>(rows + ql * OUT + (32 * b + 8 * g4 + 4 * half) * 2) = v;
     }
+  lds_exchanged();
   const int64_t pair = done ? u.pair : -1;
 #pragma unroll
   for (int c = 0; c < 32; c += G::LOAD_ROWS) {
@@ -1232,6 +1240,7 @@ __global__ __launch_bounds__(64 * kWide, 2) void wide_kernel(AttendArgs a) {
   __shared__ __attribute__((aligned(1024))) char smem[ThinShape<__bf16, D, kWide>::LDS];
   if (blockIdx.x == a.plan.thin_blocks) {
     report_entries(a, false);
+    if (a.prefix.count > 0) report_entries(a, true);
     return;
   }
   const int heads = a.shape.kv_heads, seg = blockIdx.x / heads, h = blockIdx.x - seg * heads;

@@ -315,6 +315,18 @@ def test_device_errors(gpu_lib, what, dtype):
         assert (np.abs(o[0] - ref[0]) <= tol[0]).all()
 
 
+def test_errors_of_prefixes_bounded_by_nothing(gpu_lib):
+    """Groups' entries are looked at also where the prefixes' bound leaves them no token."""
+    for what, want in (("len", sp.SP_DEV_GROUP_TOO_LARGE), ("group", sp.SP_DEV_BAD_OFFSETS)):
+        b = Batch([1, 1], [50, 40], heads=(4, 2), D=64, prefix=[20], cuts=[0, 2], seed=6)
+        b.upload(max_prefix=0)
+        if what == "group":
+            b.d_plens.zero_()
+            b.d_off[1] = 3
+        b.attend(check=False)
+        assert sp.stepprune_read_device_error(b.ws) == want
+
+
 def test_other_stream_and_graph(gpu_lib):
     """A captured call replays on lengths that grow within the bounds, with eager work
     between the replays."""
