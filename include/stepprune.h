@@ -566,8 +566,9 @@ enum { SP_ATTEND_ALL = 1u };  /* every row sees its sequence's whole run */
  * Tokens that a row does not see are no part of its sums, whatever their pages
  * hold (infinite or NaN values of tokens that only later rows see change the
  * order of the sums, so their rounding).  A prefix is read once for the rows of all
- * its sequences.  With prefixes and runs of length 0 this is cross attention to the
- * prefixes.
+ * its sequences, except for few sequences on short ones and for long prompts, which are
+ * faster with it each by itself.  With prefixes and runs of length 0 this is cross
+ * attention to the prefixes.
  *
  *  Q        [rows, q_heads head_dim], row stride ldq; 16-byte aligned
  *  rows, runs   the batch's sequences (runs->count = S)

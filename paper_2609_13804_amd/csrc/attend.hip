@@ -18,7 +18,8 @@
 //
 // A sequence's pairs to a key head decide what its rows run in:
 //   up to 16          thin tiles (memory-bound: the waves split the keys); in a batch of
-//                     few and short ones wide_kernel's, with twice the waves and no parts
+//                     few and short ones wide_kernel's, with twice the waves, the prefix
+//                     beside the own run, and no parts
 //   more              tall tiles (the waves split the pairs)
 //   more than kFuse   tall tiles that take the prefix's keys first and then its own:
 //                     such a sequence fills tiles by itself, so sharing the prefix's
@@ -550,7 +551,12 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ql = lane & 15, quad = lane >> 4, r = ratio(a);
   const int chunk_keys = prefix ? a.plan.chunk_prefix : a.plan.chunk_thin;
-  const int prefix_len = prefix || g < 0 ? 0 : a.prefix.len[g];    // (used at the end)
+  const int prefix_len = prefix || g < 0 ? 0 : a.prefix.len[g];    // (used later)
+  // a wide workgroup takes the prefix too
+  const bool both = WAVES == kWide && g >= 0;
+  Places<D * (int)sizeof(T)> before = places;
+  const int step = places.stride, own_first = places.first, prefix_first = spread ? 0 : 16 * wave;
+  if (both) before.prime(a, a.prefix, g, prefix_first, step);
   // the last pair's limit is the tile's
   const int tile_end = sees(a, t, prefix, (min(t.x0 + kThin, t.pairs) - 1) / r);
   const int k0 = chunk * chunk_keys;
@@ -568,24 +574,12 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
     if (live) u = *reinterpret_cast<const u32x4_t*>(qsrc + 4 * E * s);
     q[s] = __builtin_bit_cast(vec, u);
   }
-  const int lim = live ? sees(a, t, prefix, row) : 0, lim0 = sees(a, t, prefix, t.x0 / r);
+  const int own_lim = live ? sees(a, t, prefix, row) : 0, own_lim0 = sees(a, t, prefix, t.x0 / r);
 
-  // block i of the wave: 16 keys from first + step i on
-  const int first = places.first, step = places.stride;
-  const int blocks = k1 > first ? (k1 - first + step - 1) / step : 0;
   const char* const Kc = static_cast<const char*>(a.k_cache);
   const char* const Vc = static_cast<const char*>(a.v_cache);
   struct Block {
     u32x4_t k[SH::LOADS], v[SH::LOADS];
-  };
-  // No load is left out (the waits count them): past the last block all lanes load one place.
-  auto load = [&](Block& b, int i) {
-    const int64_t at = places.of(a, t.len, h, i);
-    const uint32_t mine = i < blocks ? lane * 16 : 0, next = i < blocks ? 1024 : 0;
-#pragma unroll
-    for (int c = 0; c < SH::LOADS; ++c) b.k[c] = fetch<STREAM>(Kc + at + c * next + mine);
-#pragma unroll
-    for (int c = 0; c < SH::LOADS; ++c) b.v[c] = fetch<STREAM>(Vc + at + c * next + mine);
   };
   f32x4_t o[D / 16];
 #pragma unroll
@@ -613,90 +607,109 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
     vdst = V + lr * SH::LDS_ROW + ch * 16;
     vsrc = V + 4 * quad * SH::LDS_ROW + ql * 4;
   }
-  auto use = [&](Block& b, int i) {
-    const int kb = first + step * i;
-    f32x4_t st = {0.0f, 0.0f, 0.0f, 0.0f};
+  // keys of the tile's own run, then of the prefix
+  for (int run = 0; run < (both ? 2 : 1); ++run) {
+    const bool pre = run == 1;
+    const int len = pre ? prefix_tokens(a, g, prefix_len) : t.len;
+    const int to = pre ? len : k1, lim = pre ? len : own_lim, lim0 = pre ? len : own_lim0;
+    if (pre) places = before;
+    // block i of the wave: 16 keys from first + step i on
+    const int first = pre ? prefix_first : own_first;
+    const int blocks = to > first ? (to - first + step - 1) / step : 0;
+    // No load is left out (the waits count them): past the last block all lanes load one place.
+    auto load = [&](Block& b, int i) {
+      const int64_t at = places.of(a, len, h, i);
+      const uint32_t mine = i < blocks ? lane * 16 : 0, next = i < blocks ? 1024 : 0;
 #pragma unroll
-    for (int c = 0; c < SH::LOADS; ++c) {
-      const uint32_t to = sizeof(T) == 2 ? kdst ^ Geo<D>::kswz(SH::LOAD_ROWS * c) << 4 : kdst;
-      *(l16_t)(lds_t)(uintptr_t)(to + c * SH::LOAD_ROWS * SH::LDS_ROW) = b.k[c];
-    }
+      for (int c = 0; c < SH::LOADS; ++c) b.k[c] = fetch<STREAM>(Kc + at + c * next + mine);
 #pragma unroll
-    for (int s = 0; s < QS; ++s) {
-      const uint32_t from = sizeof(T) == 2 ? ksrc ^ s << 6 : ksrc + s * 64;
-      const vec k = __builtin_bit_cast(vec, *(l16_t)(lds_t)(uintptr_t)from);
-      if constexpr (sizeof(T) == 2) {
-        st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[s], st, 0, 0, 0);
-      } else {
+      for (int c = 0; c < SH::LOADS; ++c) b.v[c] = fetch<STREAM>(Vc + at + c * next + mine);
+    };
+    auto use = [&](Block& b, int i) {
+      const int kb = first + step * i;
+      f32x4_t st = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) st = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j], q[s][j], st, 0, 0, 0);
+      for (int c = 0; c < SH::LOADS; ++c) {
+        const uint32_t dst = sizeof(T) == 2 ? kdst ^ Geo<D>::kswz(SH::LOAD_ROWS * c) << 4 : kdst;
+        *(l16_t)(lds_t)(uintptr_t)(dst + c * SH::LOAD_ROWS * SH::LDS_ROW) = b.k[c];
       }
-    }
-    if (kb + 16 > lim0) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (kb + 4 * quad + k >= lim) st[k] = -INFINITY;
-      // past the end: zeros
+      for (int s = 0; s < QS; ++s) {
+        const uint32_t from = sizeof(T) == 2 ? ksrc ^ s << 6 : ksrc + s * 64;
+        const vec k = __builtin_bit_cast(vec, *(l16_t)(lds_t)(uintptr_t)from);
+        if constexpr (sizeof(T) == 2) {
+          st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[s], st, 0, 0, 0);
+        } else {
 #pragma unroll
-      for (int c = 0; c < SH::LOADS; ++c)
-        if (kb + SH::LOAD_ROWS * c + lr >= k1) b.v[c] = u32x4_t{0, 0, 0, 0};
-    }
-#pragma unroll
-    for (int c = 0; c < SH::LOADS; ++c)
-      *(l16_t)(lds_t)(uintptr_t)(vdst + c * SH::LOAD_ROWS * SH::LDS_ROW) = b.v[c];
-    const float bm = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3])) * c2;
-    // float32 for any, since an exponent's rounding grows with its size: error 5.7e-7, else 7.9e-7
-    if (__any(bm > m + (sizeof(T) == 2 ? kRescale : 0.0f))) {
-      const float mn = fmaxf(m, quad_max(bm));
-      const float sc = __builtin_amdgcn_exp2f(m - mn);
-      m = mn;
-      l *= sc;
-#pragma unroll
-      for (int e = 0; e < D / 16; ++e) o[e] *= sc;
-    }
-    float p[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      float e = fmaf(st[k], c2, -m);
-      // float32: with the rest of scale log2(e), whose rounding would be off by up to 2^-24 of the score
-      if (sizeof(T) == 4 && st[k] > kLowest) e = fmaf(st[k], c2_low, e);
-      p[k] = __builtin_amdgcn_exp2f(e);
-      l += p[k];
-    }
-    if constexpr (sizeof(T) == 2) {
-      bf16x4_t pb;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) pb[k] = (__bf16)p[k];
-#pragma unroll
-      for (int e = 0; e < D / 16; ++e) {
-        const bf16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((ltr_t)(lds_t)(uintptr_t)(vsrc ^ e << 5));
-        o[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, v),
-                                                         __builtin_bit_cast(s16x4_t, pb), o[e], 0, 0, 0);
+          for (int j = 0; j < 4; ++j) st = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j], q[s][j], st, 0, 0, 0);
+        }
       }
-    } else {
-#pragma unroll
-      for (int e = 0; e < D / 16; ++e)
+      if (kb + 16 > lim0) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(*(l4_t)(lds_t)(uintptr_t)(vsrc + k * SH::LDS_ROW + e * 64), p[k],
-                                                      o[e], 0, 0, 0);
-    }
-  };
-  if (blocks > 0) {
-    Block b[SH::DEPTH];
+          if (kb + 4 * quad + k >= lim) st[k] = -INFINITY;
+        // past the end: zeros
 #pragma unroll
-    for (int j = 0; j < SH::DEPTH; ++j) load(b[j], j);
-    for (int i = 0; i < blocks; i += SH::DEPTH) {
+        for (int c = 0; c < SH::LOADS; ++c)
+          if (kb + SH::LOAD_ROWS * c + lr >= to) b.v[c] = u32x4_t{0, 0, 0, 0};
+      }
 #pragma unroll
-      for (int j = 0; j < SH::DEPTH; ++j) {
-        if (i + j < blocks) use(b[j], i + j);
-        load(b[j], i + j + SH::DEPTH);
+      for (int c = 0; c < SH::LOADS; ++c)
+        *(l16_t)(lds_t)(uintptr_t)(vdst + c * SH::LOAD_ROWS * SH::LDS_ROW) = b.v[c];
+      const float bm = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3])) * c2;
+      // float32 for any, since an exponent's rounding grows with its size: error 5.7e-7, else 7.9e-7
+      if (__any(bm > m + (sizeof(T) == 2 ? kRescale : 0.0f))) {
+        const float mn = fmaxf(m, quad_max(bm));
+        const float sc = __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= sc;
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) o[e] *= sc;
+      }
+      float p[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float e = fmaf(st[k], c2, -m);
+        // float32: with the rest of scale log2(e), whose rounding would be off by up to 2^-24 of the score
+        if (sizeof(T) == 4 && st[k] > kLowest) e = fmaf(st[k], c2_low, e);
+        p[k] = __builtin_amdgcn_exp2f(e);
+        l += p[k];
+      }
+      if constexpr (sizeof(T) == 2) {
+        bf16x4_t pb;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) pb[k] = (__bf16)p[k];
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) {
+          const bf16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((ltr_t)(lds_t)(uintptr_t)(vsrc ^ e << 5));
+          o[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, v),
+                                                           __builtin_bit_cast(s16x4_t, pb), o[e], 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(*(l4_t)(lds_t)(uintptr_t)(vsrc + k * SH::LDS_ROW + e * 64), p[k],
+                                                        o[e], 0, 0, 0);
+      }
+    };
+    if (blocks > 0) {
+      Block b[SH::DEPTH];
+#pragma unroll
+      for (int j = 0; j < SH::DEPTH; ++j) load(b[j], j);
+      for (int i = 0; i < blocks; i += SH::DEPTH) {
+#pragma unroll
+        for (int j = 0; j < SH::DEPTH; ++j) {
+          if (i + j < blocks) use(b[j], i + j);
+          load(b[j], i + j + SH::DEPTH);
+        }
       }
     }
   }
   l = quad_sum(l);
   float finite = 0.0f;                               // NaN: no
-  if (lim0 < k1) {                                   // some pairs do not see all keys
+  if (own_lim0 < k1) {                               // some pairs do not see all keys
 #pragma unroll
     for (int e = 0; e < D / 16; ++e)
 #pragma unroll
@@ -704,17 +717,16 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
   }
   if (__any(finite != 0.0f)) {
     KeyByKey<T, D, 16, 4, decltype(o)> kk(o, m, l);
-    for (int i = 0; i < blocks; ++i) {
-      const int kb = first + step * i;
-      kk.add(a, t.table, h, q, kb, min(kb + 16, k1), lim);
-    }
+    for (int kb = own_first; kb < k1; kb += step) kk.add(a, t.table, h, q, kb, min(kb + 16, k1), own_lim);
+    const int len = both ? prefix_tokens(a, g, prefix_len) : 0;
+    for (int kb = prefix_first; kb < len; kb += step) kk.add(a, pages_of(a, true, g), h, q, kb, min(kb + 16, len), len);
   }
 
   typedef T out4_t __attribute__((ext_vector_type(4)));
-  const int pre = ceil_div(prefix_tokens(a, g, prefix_len), a.plan.chunk_prefix);
+  const int pre = WAVES == kWide ? 0 : ceil_div(prefix_tokens(a, g, prefix_len), a.plan.chunk_prefix);
   if (spread) {
     if (!live) return;
-    const Out u = own_place(a, t, h, x, chunk, ceil_div(lim, chunk_keys), pre);
+    const Out u = own_place(a, t, h, x, chunk, ceil_div(own_lim, chunk_keys), pre);
     if (u.pair < 0) return;
     if (quad == 0) store_ml(a, u, m, l);
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -1234,7 +1246,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 && D == 64 ? 3 : 2) voi
 }
 
 // Few sequences, of at most 16 pairs and not too many keys: eight waves to a sequence and key
-// head, so that no parts are left for a second launch to join.
+// head, over its own run and its prefix, so that no parts are left for a second launch to join.
 template <int D>
 __global__ __launch_bounds__(64 * kWide, 2) void wide_kernel(AttendArgs a) {
   __shared__ __attribute__((aligned(1024))) char smem[ThinShape<__bf16, D, kWide>::LDS];
@@ -1249,7 +1261,7 @@ __global__ __launch_bounds__(64 * kWide, 2) void wide_kernel(AttendArgs a) {
   Tile t;
   int g;
   if (!sequence_tile(a, seg, t, g)) return;
-  thin_tile<__bf16, D, true, kWide>(a, smem, false, t, places, h, 0, -1, false);
+  thin_tile<__bf16, D, true, kWide>(a, smem, false, t, places, h, 0, g, false);
 }
 
 // ---------------------------------------------------------------- joining the parts
@@ -1445,9 +1457,15 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
   //   256 of 64, 256, 707, 2048        6.7 / 6.3, 10.3 / 9.9, 23.1 / 19.8, 53.7 / 49.2
   //   512 of 64, 256, 707              8.5 / 9.9, 15.7 / 17.5, 35.3 / 36.4
   // float32's products take a compute unit too long: 16 of 640 tokens, heads of 64, 10.4 / 11.5.
-  const int64_t items = S * heads;
-  p.wide = !f32 && !own_tall && prefix.max_len == 0 && items <= 256 &&
-           runs.max_len <= (items <= 64 ? 512 : items <= 192 ? 768 : 2048);
+  // With prefixes of 256, 400, 700, 1000 tokens before up to 64 own ones, shared and joined /
+  // taken by each sequence:
+  //   16 sequences on 1 prefix, 4 key heads    13.2 / 8.1, 14.4 / 9.4
+  //   64 on 4, 4 key heads                     16.3 / 9.6, 17.6 / 11.1, 18.9 / 13.8, 20.4 / 16.9
+  //    8 on 1, 32 key heads                    11.9 / 8.7, 13.0 / 10.3, 12.7 / 12.5, 13.1 / 15.3
+  const int before = G > 0 ? prefix.max_len : 0;
+  const int64_t items = S * heads, together = (int64_t)runs.max_len + before;
+  p.wide = !f32 && !own_tall && items <= 256 &&
+           together <= (items <= 64 ? 512 : items <= 192 ? 768 : before > 0 ? 1024 : 2048);
   if (p.wide) {
     p.spread = 0;
     p.chunk_thin = (runs.max_len / (16 * kWide) + 1) * 16 * kWide;

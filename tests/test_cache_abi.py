@@ -135,8 +135,10 @@ def test_workspace_query(sp):
                                                          kw.pop("runs", _runs(sp)), kw.pop("prefix", None))
     base = ws()
     assert base >= 256 + 4 * 4
-    # one part to a row and prefix: m, l and the output of every (row, head)
-    assert ws(prefix=_runs(sp, count=1)) >= 256 + 4 * 4 + 4 * 8 * 2 * (128 + 2) * 4
+    # few sequences take a short prefix by themselves: no parts; of a long one, a part of the
+    # prefix and of the row's own run: m, l and the output of every (row, head)
+    assert ws(prefix=_runs(sp, count=1)) == base
+    assert ws(prefix=_runs(sp, count=1, width=1 << 10, max_len=4096)) >= 256 + 4 * 4 + 4 * 8 * 2 * (128 + 2) * 4
     long = _runs(sp, count=1, width=1 << 16, max_len=1 << 20)
     assert ws(runs=long) > base
     for kw, _ in DIMS:

@@ -388,3 +388,26 @@ def test_two_streams_at_once(gpu_lib):
     torch.cuda.synchronize()
     for b, o, out in zip(batches, alone, outs):
         assert np.array_equal(out.double().cpu().numpy().reshape(o.shape)[b.live()], o[b.live()])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("layout", ["packed", "padded"])
+@pytest.mark.parametrize("prefix", [[1, 0, 129], [128, 400, 17], [500, 3, 383]])
+def test_few_sequences_with_their_prefixes(gpu_lib, D, layout, prefix):
+    """Few sequences that each take their prefix themselves: groups of several and of none,
+    sequences outside every group, runs of no token, rows whose last token is NaN for the
+    last of them alone, NaN behind every run's and prefix's end."""
+    counts, lens = [1, 4, 1, 0, 3, 1, 4], [90, 4, 0, 5, 100, 17, 60]
+    b = Batch(counts, lens, heads=(8, 2), D=D, layout=layout, prefix=prefix, cuts=[1, 3, 3, 6], pad=1, seed=D)
+    b.upload()
+    clean, _ = b.attend()
+    b.check(clean, _)
+    b.check(*b.attend(see_all=True), see_all=True)
+    tol, _ = b.bounds(*b.oracle())
+    b.v_cache[b.tables[4][99 // 16], :, 99 % 16] = np.inf
+    b.upload()
+    o, _ = b.attend()
+    last = b.first[4] + 2
+    assert not np.isfinite(o[last]).any()
+    rows = np.setdiff1d(b.live(), [last])
+    assert np.isfinite(o[rows]).all() and (np.abs(o[rows] - clean[rows]) <= 2 * tol[rows]).all()
