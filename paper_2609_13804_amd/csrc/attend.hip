@@ -24,6 +24,7 @@
 //   more than kFuse   tall tiles that take the prefix's keys first and then its own:
 //                     such a sequence fills tiles by itself, so sharing the prefix's
 //                     reads saves nothing and parts would only be written and read.
+// Where most are more than 16, all take their prefixes so (ALONE).
 #include <float.h>
 
 #include <algorithm>
@@ -169,6 +170,7 @@ __device__ __forceinline__ void find_prefix(const AttendArgs& a, Tile& t) {
 // of the batch 154 us, in this one 137.)
 constexpr int kSorted = 64;
 // LDS: kSorted entries of `table`, the wave's own.
+template <bool ALONE>
 __device__ __forceinline__ bool find_sorted_tile(const AttendArgs& a, bool prefix, int index, Tile& t, uint2* table) {
   const int lane = threadIdx.x & 63, r = ratio(a), G = a.prefix.count;
   const CacheRuns& runs = prefix ? a.prefix : a.runs;
@@ -206,7 +208,7 @@ __device__ __forceinline__ bool find_sorted_tile(const AttendArgs& a, bool prefi
     tokens = prefix_tokens(a, group, tokens);
   }
   // order: keys, then the place in the batch
-  const uint32_t keys = (uint32_t)len + (grouped && n * r > kFuse ? (uint32_t)tokens : 0);
+  const uint32_t keys = (uint32_t)len + (grouped && (ALONE || n * r > kFuse) ? (uint32_t)tokens : 0);
   const uint32_t order = min(keys, (1u << 26) - 1) << 6 | (63 - lane);
   table[lane] = make_uint2(order, (uint32_t)tiles);
   lds_exchanged();
@@ -542,7 +544,7 @@ __device__ __forceinline__ u32x4_t fetch(const char* p) {
   else return *reinterpret_cast<const u32x4_t*>(p);
 }
 
-template <typename T, int D, bool STREAM, int WAVES>
+template <typename T, int D, bool STREAM, int WAVES, bool ALONE>
 __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool prefix, const Tile& t,
                                           Places<D * (int)sizeof(T)>& places, int h, int chunk, int g, bool spread) {
   using SH = ThinShape<T, D, WAVES>;
@@ -552,8 +554,8 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
   const int ql = lane & 15, quad = lane >> 4, r = ratio(a);
   const int chunk_keys = prefix ? a.plan.chunk_prefix : a.plan.chunk_thin;
   const int prefix_len = prefix || g < 0 ? 0 : a.prefix.len[g];    // (used later)
-  // a wide workgroup takes the prefix too
-  const bool both = WAVES == kWide && g >= 0;
+  // a tile that takes the prefix too, with its first keys
+  const bool both = ALONE && chunk == 0 && g >= 0;
   Places<D * (int)sizeof(T)> before = places;
   const int step = places.stride, own_first = places.first, prefix_first = spread ? 0 : 16 * wave;
   if (both) before.prime(a, a.prefix, g, prefix_first, step);
@@ -723,7 +725,7 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
   }
 
   typedef T out4_t __attribute__((ext_vector_type(4)));
-  const int pre = WAVES == kWide ? 0 : ceil_div(prefix_tokens(a, g, prefix_len), a.plan.chunk_prefix);
+  const int pre = ALONE ? 0 : ceil_div(prefix_tokens(a, g, prefix_len), a.plan.chunk_prefix);
   if (spread) {
     if (!live) return;
     const Out u = own_place(a, t, h, x, chunk, ceil_div(own_lim, chunk_keys), pre);
@@ -960,7 +962,7 @@ __device__ __forceinline__ float pipeline_step(Pairs<D>& w, f32x16_t (&st)[2], u
 // the vector units weigh one step's scores, the next step's are on the matrix cores.
 // Keys: a fused tile takes its prefix's steps first (the last one may be ragged), then
 // its own run's.
-template <int D>
+template <int D, bool ALONE>
 __device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool prefix, const Tile& t, int h, int chunk) {
   using G = Geo<D>;
   constexpr int STEP = kTallStep * G::ROW;                                    // 64 keys of K or V
@@ -969,7 +971,7 @@ __device__ __forceinline__ void tall_tile(const AttendArgs& a, char* smem, bool 
   int g = -1, pre = 0, P = 0;                        // parts of the prefix apart; its tokens taken here
   if (!prefix) {
     g = t.group;
-    if (t.pairs > kFuse) P = t.before;
+    if (ALONE || t.pairs > kFuse) P = t.before;
     else pre = ceil_div(t.before, a.plan.chunk_prefix);
   }
   const int before = ceil_div(P, kTallStep);
@@ -1186,7 +1188,8 @@ __device__ __forceinline__ bool sequence_tile(const AttendArgs& a, int seg, Tile
 // One launch for all tiles: the prefixes' (thin or tall), the sequences' tall ones, the
 // sequences' thin ones, in this order; the last workgroup looks for errors in the batch's
 // entries, wherever they are.  float32 has thin tiles only, several to a longer sequence.
-template <typename T, int D, bool STREAM>
+// ALONE: no sequence shares its prefix's tiles.
+template <typename T, int D, bool STREAM, bool ALONE>
 __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 && D == 64 ? 3 : 2) void attend_kernel(AttendArgs a) {
   constexpr bool BF16 = sizeof(T) == 2;
   // the tall tiles' two steps of K and of V: two workgroups to a compute unit, or (D 64) three
@@ -1203,7 +1206,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 && D == 64 ? 3 : 2) voi
   Tile t;
   // block id of `tiles` tiles, the key heads and the chunks
   if constexpr (BF16) {
-    const bool prefix = p.prefix_tall && id < p.prefix_blocks;
+    const bool prefix = !ALONE && p.prefix_tall && id < p.prefix_blocks;
     if (prefix || (id >= p.prefix_blocks && id < p.prefix_blocks + p.tall_blocks)) {
       if (!prefix) id -= p.prefix_blocks;
       const int tiles = prefix ? p.prefix_tiles : p.tall_tiles;
@@ -1214,17 +1217,17 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 && D == 64 ? 3 : 2) voi
       if ((prefix ? a.prefix.count : a.runs.count) <= kSorted) {
         // (the last quarter of the tall tiles' LDS: not written before their first barrier)
         uint2* const table = reinterpret_cast<uint2*>(smem + 6 * kTallStep * D) + kSorted * ((int)threadIdx.x >> 6);
-        if (!find_sorted_tile(a, prefix, tile, t, table)) return;
+        if (!find_sorted_tile<ALONE>(a, prefix, tile, t, table)) return;
       } else {
         if (!find_tile<kTall>(a, prefix, tiles - 1 - tile, t)) return;
         if (!prefix && t.pairs <= kThin) return;                             // a thin tile's
         if (!prefix) find_prefix(a, t);
       }
-      tall_tile<D>(a, smem, prefix, t, h, chunk);
+      tall_tile<D, ALONE>(a, smem, prefix, t, h, chunk);
       return;
     }
   }
-  const bool prefix = id < p.prefix_blocks;
+  const bool prefix = !ALONE && id < p.prefix_blocks;
   if (!prefix) id -= p.prefix_blocks + p.tall_blocks;
   const bool spread = !prefix && p.spread;
   const int tiles = prefix ? p.prefix_tiles : p.thin_tiles;
@@ -1242,7 +1245,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 && D == 64 ? 3 : 2) voi
     places.prime(a, a.runs, tile, key, spread ? 16 : kThinStep);
     if (!sequence_tile(a, tile, t, g)) return;
   }
-  thin_tile<T, D, STREAM, kWaves>(a, smem, prefix, t, places, h, chunk, g, spread);
+  thin_tile<T, D, STREAM, kWaves, ALONE>(a, smem, prefix, t, places, h, chunk, g, spread);
 }
 
 // Few sequences, of at most 16 pairs and not too many keys: eight waves to a sequence and key
@@ -1261,7 +1264,7 @@ __global__ __launch_bounds__(64 * kWide, 2) void wide_kernel(AttendArgs a) {
   Tile t;
   int g;
   if (!sequence_tile(a, seg, t, g)) return;
-  thin_tile<__bf16, D, true, kWide>(a, smem, false, t, places, h, 0, g, false);
+  thin_tile<__bf16, D, true, kWide, true>(a, smem, false, t, places, h, 0, g, false);
 }
 
 // ---------------------------------------------------------------- joining the parts
@@ -1440,6 +1443,13 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
   p.by_row = longest <= p.short_pairs;
   p.short_rows = (int)((p.short_pairs + r - 1) / r);
   p.thin_tiles = (int)(p.thin_tiled ? pairs / kThin + S : S);
+  // Prompts are faster with their prefixes each by itself, however short (no tiles of the
+  // prefixes, no parts to write and to join); many single tokens beside a few prompts are not.
+  // us, prefixes of 64, 256, 1024 tokens, shared / each by itself: 64 prompts of 24 to 96 rows
+  // on 4, 28 heads on 4, 43.5 / 34.4, 54.3 / 45.2, 99.1 / 92.2; of 3 to 12 rows 23.7 / 13.1,
+  // 28.6 / 16.5, 46.1 / 28.4; 64 of 20 to 60 on 8, 32 heads, 120 / 57, 131 / 76, 185 / 152.
+  // 128 single tokens on 8 prefixes of 64, 256: 30.5 / 34.4, 34.0 / 58.8.
+  p.alone = own_tall && G > 0 && pairs >= kThin * S;
   // A wave to a head, where there are heads enough to fill the device and the runs are short:
   // fewer workgroups to begin and end, less even work.  us, four waves / one to a head, runs of 5,
   // 64, 128, 192, 256 tokens, heads of 128: 576 runs and key heads 9.6 / 6.1, 9.9 / 7.6,
@@ -1484,7 +1494,7 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
     p.tall_blocks = p.tall_tiles * heads * (p.tall_parts > 0 ? p.tall_parts : 1);
     if (p.tall_parts > p.short_parts) p.short_parts = p.tall_parts;
   }
-  if (G > 0 && prefix.max_len > 0) {
+  if (G > 0 && prefix.max_len > 0 && !p.alone) {
     p.prefix_tall = !f32 && pairs > kThin * G;
     p.prefix_tiles = (int)(pairs / (p.prefix_tall ? kTall : kThin) + G);
     p.chunk_prefix = p.prefix_tall
@@ -1527,10 +1537,11 @@ void launch_attend(const AttendArgs& a, hipStream_t stream) {
   const AttendPlan& p = a.plan;
   const dim3 grid((unsigned)(p.prefix_blocks + p.tall_blocks + p.thin_blocks + 1)), block(64 * kWaves);
   if (p.wide) hipLaunchKernelGGL((wide_kernel<D>), grid, dim3(64 * kWide), 0, stream, a);
+  else if (p.alone) hipLaunchKernelGGL((attend_kernel<__bf16, D, true, true>), grid, block, 0, stream, a);
   else if (std::is_same<T, float>::value && p.reread)
-    hipLaunchKernelGGL((attend_kernel<float, D, false>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((attend_kernel<float, D, false, false>), grid, block, 0, stream, a);
   else
-    hipLaunchKernelGGL((attend_kernel<T, D, true>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((attend_kernel<T, D, true, false>), grid, block, 0, stream, a);
   const int64_t first = short_join_blocks(a), second = tall_join_blocks(a);
   if (first + second == 0) return;
   const dim3 joins((unsigned)(first + second));

@@ -223,6 +223,7 @@ struct AttendPlan {
   int prefix_tall;                                  // the prefixes' tiles are tall ones
   int spread;                                       // thin tiles: a wave to a key head, not four
   int wide;                                         // thin tiles only, each of a wide workgroup, no parts
+  int alone;                                        // each sequence's tiles take its prefix themselves
   int thin_tiled;                                   // sequences have several thin tiles
   int reread;                                       // thin tiles read the same keys
   int prefix_tiles, tall_tiles, thin_tiles;         // tiles of a key head
