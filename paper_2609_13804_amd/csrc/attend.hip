@@ -24,7 +24,7 @@
 //   more than kFuse   tall tiles that take the prefix's keys first and then its own:
 //                     such a sequence fills tiles by itself, so sharing the prefix's
 //                     reads saves nothing and parts would only be written and read.
-// Where most are more than 16, all take their prefixes so (ALONE).
+// Where that is less work, all sequences of a batch take their prefixes so (ALONE).
 #include <float.h>
 
 #include <algorithm>
@@ -1443,13 +1443,22 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
   p.by_row = longest <= p.short_pairs;
   p.short_rows = (int)((p.short_pairs + r - 1) / r);
   p.thin_tiles = (int)(p.thin_tiled ? pairs / kThin + S : S);
-  // Prompts are faster with their prefixes each by itself, however short (no tiles of the
-  // prefixes, no parts to write and to join); many single tokens beside a few prompts are not.
-  // us, prefixes of 64, 256, 1024 tokens, shared / each by itself: 64 prompts of 24 to 96 rows
-  // on 4, 28 heads on 4, 43.5 / 34.4, 54.3 / 45.2, 99.1 / 92.2; of 3 to 12 rows 23.7 / 13.1,
-  // 28.6 / 16.5, 46.1 / 28.4; 64 of 20 to 60 on 8, 32 heads, 120 / 57, 131 / 76, 185 / 152.
-  // 128 single tokens on 8 prefixes of 64, 256: 30.5 / 34.4, 34.0 / 58.8.
-  p.alone = own_tall && G > 0 && pairs >= kThin * S;
+  // Prompts take their prefixes each by itself (no tiles of the prefixes, no parts to write and
+  // to join) unless that is more work: the steps of tall tiles that sharing would fill and they
+  // do not, against the parts.  By the rows' mean, and what was measured: us, shared / each by
+  // itself, prefixes of 64, 256, 1024, 2000 tokens, heads of 128:
+  //   64 prompts of 24 to 96 rows on 4, 28 heads on 4   43 / 33, 53 / 44, 103 / 93, 154 / 144
+  //   64 of 3 to 12 on 4, 28 heads on 4                 24 / 13, 29 / 16, 46 / 27, 63 / 43
+  //   64 of 2 to 8 on 4, 28 heads on 4                  20 / 13, 23 / 16, 27 / 31, 36 / 57
+  //   64 of 20 to 60 on 8, 32 heads                     118 / 54, 129 / 71, 188 / 153, 263 / 273
+  //   32 of 1 to 40 on 4, 32 heads                      36 / 25, 40 / 44, 57 / 117, 72 / 206
+  //   100 of 1 to 10 on 4, 32 heads on 8                32 / 24, 35 / 39, 43 / 106, 52 / 164
+  if (own_tall && G > 0 && prefix.max_len > 0) {
+    const double unfilled = std::max(0.0, (double)S - (double)pairs / kTall) * (double)heads;
+    const double steps = (double)((prefix.max_len + kTallStep - 1) / kTallStep);
+    const double parts = 5.0 + (double)(pairs * heads) * s.head_dim * 8.0 / 2.0e6;
+    p.alone = unfilled * steps * 0.0045 * s.head_dim / 128.0 < parts;
+  }
   // A wave to a head, where there are heads enough to fill the device and the runs are short:
   // fewer workgroups to begin and end, less even work.  us, four waves / one to a head, runs of 5,
   // 64, 128, 192, 256 tokens, heads of 128: 576 runs and key heads 9.6 / 6.1, 9.9 / 7.6,
