@@ -296,22 +296,30 @@ def cache_dims(q_heads, kv_heads, head_dim, dtype, page_size, pages) -> sp_cache
     return sp_cache_dims(q_heads, kv_heads, head_dim, dtype, page_size, pages)
 
 
+def _keeping(struct, *tensors):
+    """The struct, with the tensors whose addresses it holds: they live as long as it does."""
+    struct.tensors = tensors
+    return struct
+
+
 def cache_rows(rows, layout, rows_per_seq, seq_info, max_rows) -> sp_cache_rows:
     """The rows of a batch (``seq_info`` device int32, as the compaction writes it)."""
-    return sp_cache_rows(rows, layout, rows_per_seq, _ptr(seq_info), max_rows)
+    return _keeping(sp_cache_rows(rows, layout, rows_per_seq, _ptr(seq_info), max_rows), seq_info)
 
 
 def cache_runs(table, length, max_len) -> sp_cache_runs:
     """Runs of the cache: device int32 ``table`` [count, width] and ``length`` [count]."""
-    return sp_cache_runs(_ptr(table), _ptr(length), table.shape[0], table.shape[1], max_len)
+    return _keeping(sp_cache_runs(_ptr(table), _ptr(length), table.shape[0], table.shape[1], max_len), table,
+                    length)
 
 
 def cache_rotation(cos_sin, rot_dim, pos=None, section=None, interleaved=False) -> sp_cache_rotation:
     """Rotation by position: float32 ``cos_sin`` [positions, rot_dim / 2, 2]; int32 ``pos``
     [axes, rows] with the pairs of each axis in ``section``, or None: the rows' slots."""
     section = [rot_dim // 2] if section is None else list(section)
-    return sp_cache_rotation(_ptr(cos_sin), cos_sin.shape[0], rot_dim, 1 if interleaved else 0, _ptr(pos),
-                             len(section), (_I32 * 3)(*(section + [0] * (3 - len(section)))))
+    return _keeping(sp_cache_rotation(_ptr(cos_sin), cos_sin.shape[0], rot_dim, 1 if interleaved else 0,
+                                      _ptr(pos), len(section), (_I32 * 3)(*(section + [0] * (3 - len(section))))),
+                    cos_sin, pos)
 
 
 def _ref(struct):
