@@ -296,6 +296,15 @@ def cache_dims(q_heads, kv_heads, head_dim, dtype, page_size, pages) -> sp_cache
     return sp_cache_dims(q_heads, kv_heads, head_dim, dtype, page_size, pages)
 
 
+def _read_as(what, t, dtype, at_least):
+    """A tensor of a struct's array: the struct has its address only, so another type, or rows
+    that are apart, would be read as something else.  (Raw addresses pass.)"""
+    if hasattr(t, "is_contiguous") and (str(t.dtype) != f"torch.{dtype}" or not t.is_contiguous() or
+                                        t.numel() < at_least):
+        raise ValueError(f"{what}: contiguous {dtype} of at least {at_least} elements, not {t.dtype} of shape "
+                         f"{tuple(t.shape)} and strides {t.stride()}")
+
+
 def _keeping(struct, *tensors):
     """The struct, with the tensors whose addresses it holds: they live as long as it does."""
     struct.tensors = tensors
@@ -304,11 +313,16 @@ def _keeping(struct, *tensors):
 
 def cache_rows(rows, layout, rows_per_seq, seq_info, max_rows) -> sp_cache_rows:
     """The rows of a batch (``seq_info`` device int32, as the compaction writes it)."""
+    _read_as("seq_info", seq_info, "int32", 0)
     return _keeping(sp_cache_rows(rows, layout, rows_per_seq, _ptr(seq_info), max_rows), seq_info)
 
 
 def cache_runs(table, length, max_len) -> sp_cache_runs:
     """Runs of the cache: device int32 ``table`` [count, width] and ``length`` [count]."""
+    if len(table.shape) != 2:
+        raise ValueError(f"table: [count, width], not {tuple(table.shape)}")
+    _read_as("table", table, "int32", 0)
+    _read_as("length", length, "int32", table.shape[0])
     return _keeping(sp_cache_runs(_ptr(table), _ptr(length), table.shape[0], table.shape[1], max_len), table,
                     length)
 
@@ -317,6 +331,12 @@ def cache_rotation(cos_sin, rot_dim, pos=None, section=None, interleaved=False) 
     """Rotation by position: float32 ``cos_sin`` [positions, rot_dim / 2, 2]; int32 ``pos``
     [axes, rows] with the pairs of each axis in ``section``, or None: the rows' slots."""
     section = [rot_dim // 2] if section is None else list(section)
+    _read_as("cos_sin", cos_sin, "float32", 0)
+    if hasattr(cos_sin, "numel") and cos_sin.numel() != cos_sin.shape[0] * rot_dim:
+        raise ValueError(f"cos_sin: [positions, {rot_dim // 2}, 2], not {tuple(cos_sin.shape)}")
+    _read_as("pos", pos, "int32", 0)
+    if hasattr(pos, "shape") and (1 if len(pos.shape) == 1 else pos.shape[0]) != len(section):
+        raise ValueError(f"pos: [{len(section)}, rows], not {tuple(pos.shape)}")
     return _keeping(sp_cache_rotation(_ptr(cos_sin), cos_sin.shape[0], rot_dim, 1 if interleaved else 0,
                                       _ptr(pos), len(section), (_I32 * 3)(*(section + [0] * (3 - len(section))))),
                     cos_sin, pos)
