@@ -198,11 +198,17 @@ class DeviceRun:
         """Positions of the compacted buffer's rows, [axes, out_rows] int32, from the
         tokens' own (``vis_pos`` [axes, T_vis], ``text_pos`` [axes, T_txt], int32 on the
         device): what the rotation of their keys takes.  Zero where the buffer has no row."""
-        s = self.sizes
+        s, axes = self.sizes, vis_pos.shape[0]
         if pos is None:
-            pos = torch.zeros((vis_pos.shape[0], self.out_rows), dtype=torch.int32, device=self.X.device)
+            pos = torch.zeros((axes, self.out_rows), dtype=torch.int32, device=self.X.device)
+        # (the launch has the addresses and these sizes only)
+        for name, t, columns in (("vis_pos", vis_pos, s.T_vis), ("text_pos", text_pos, s.T_txt),
+                                 ("pos", pos, self.out_rows)):
+            if tuple(t.shape) != (axes, columns) or t.dtype != torch.int32 or not t.is_contiguous():
+                raise ValueError(f"{name}: contiguous int32 [{axes}, {columns}], not {t.dtype} of shape "
+                                 f"{tuple(t.shape)} and strides {t.stride()}")
         sp.stepprune_compact_positions(vis_pos, s.T_vis, self.img_off, text_pos, s.T_txt, self.text_off,
-                                       vis_pos.shape[0], self.kept_idx, self.kept_off, self.kept_cnt, s.B,
+                                       axes, self.kept_idx, self.kept_off, self.kept_cnt, s.B,
                                        self.layout_code, self.rows_per_image, self.out_rows, pos,
                                        self.ws[2], self.ws_bytes[2], stream)
         return pos
