@@ -4,6 +4,7 @@
 Plumbing only: torch allocates HBM and provides the streams and events; every
 stage runs in libstepprune's kernels through the binding.
 """
+import contextlib
 import copy
 import os
 from dataclasses import dataclass
@@ -36,6 +37,15 @@ def _storage_rows(a: np.ndarray) -> np.ndarray:
     of storage, because the ABI takes a valid E_text pointer (no kernel reads
     a row outside the ones text_off spans)."""
     return a if a.shape[0] > 0 else np.zeros((1,) + a.shape[1:], a.dtype)
+
+
+def _on(stream, device):
+    """The context of a stream as the calls take one: None (the current), torch's or a raw handle."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
+    return torch.cuda.stream(stream)
 
 
 class DeviceRun:
@@ -197,10 +207,14 @@ class DeviceRun:
     def positions(self, vis_pos, text_pos, pos=None, stream=None):
         """Positions of the compacted buffer's rows, [axes, out_rows] int32, from the
         tokens' own (``vis_pos`` [axes, T_vis], ``text_pos`` [axes, T_txt], int32 on the
-        device): what the rotation of their keys takes.  Zero where the buffer has no row."""
+        device): what the rotation of their keys takes.  Without ``pos`` the array is made here,
+        on the launch's stream, and zero where the buffer has no row."""
         s, axes = self.sizes, vis_pos.shape[0]
         if pos is None:
-            pos = torch.zeros((axes, self.out_rows), dtype=torch.int32, device=self.X.device)
+            with _on(stream, self.X.device):
+                pos = torch.zeros((axes, self.out_rows), dtype=torch.int32, device=self.X.device)
+            if stream is not None:                   # (the block is that stream's; the caller's may read it)
+                pos.record_stream(torch.cuda.current_stream(self.X.device))
         # (the launch has the addresses and these sizes only)
         for name, t, columns in (("vis_pos", vis_pos, s.T_vis), ("text_pos", text_pos, s.T_txt),
                                  ("pos", pos, self.out_rows)):
