@@ -565,10 +565,14 @@ enum { SP_ATTEND_ALL = 1u };  /* every row sees its sequence's whole run */
  * A row that sees no token (or only scores of -inf) gives o = 0, lse = -inf.
  * Tokens that a row does not see are no part of its sums, whatever their pages
  * hold (infinite or NaN values of tokens that only later rows see change the
- * order of the sums, so their rounding).  A prefix is read once for the rows of all
- * its sequences, except for few sequences on short ones and for long prompts, which are
- * faster with it each by itself.  With prefixes and runs of length 0 this is cross
+ * order of the sums, so their rounding).  With prefixes and runs of length 0 this is cross
  * attention to the prefixes.
+ *
+ * A prefix is read once for the rows of all its sequences, except where reading it for each
+ * is faster, by the bounds: for few sequences of up to 16 rows x (q_heads / kv_heads) on short
+ * prefixes; for a sequence of more than 64 of them; and, where the longest sequence has more than
+ * 16, for all sequences of the batch, unless their short ones would read long prefixes many
+ * times or end behind the long ones.
  *
  *  Q        [rows, q_heads head_dim], row stride ldq; 16-byte aligned
  *  rows, runs   the batch's sequences (runs->count = S)

@@ -1435,6 +1435,8 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
   const int64_t heads = s.kv_heads, S = runs.count, G = prefix.count;
   const bool f32 = s.dtype == SP_F32;
   const bool own_tall = !f32 && longest > kThin;
+  // keys of a tall tile, the prefix's in whole steps
+  const int64_t tall_keys = (prefix.max_len + kTallStep - 1) / kTallStep * kTallStep + (int64_t)runs.max_len;
   p.thin_tiled = f32 && longest > kThin;
   p.reread = p.thin_tiled || (f32 && G > 0 && pairs > kThin * G);
   // float32 has no tall tiles: every sequence is short, and its prefix is shared
@@ -1453,18 +1455,40 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
   //   64 of 20 to 60 on 8, 32 heads                     118 / 54, 129 / 71, 188 / 153, 263 / 273
   //   32 of 1 to 40 on 4, 32 heads                      36 / 25, 40 / 44, 57 / 117, 72 / 206
   //   100 of 1 to 10 on 4, 32 heads on 8                32 / 24, 35 / 39, 43 / 106, 52 / 164
+  // Single tokens beside long prompts have no place in that mean, but would take the whole prefix
+  // in one workgroup each.  `most` sequences can be that short, where all others are as long as
+  // the longest; in an even batch half of them would be, so those past half are taken to be
+  // (`thin`).  Their steps fill what the tall tiles leave of the device, at half the cost; and one
+  // such workgroup, at 0.6 us a step (heads of 64: 0.37), is to end before the tall tiles' chunks.
+  // us, shared / each by itself, 28 heads of 128 on 4:
+  //   one prompt of 40 rows and 1 token, on 1024, 2000, 8192 tokens      18 / 21, 21 / 30, 31 / 87
+  //   of 512 rows and 1, on 2000, 8192, 131072                           50 / 44, 87 / 120, 968 / 1590
+  //   of 512 and 16, on 1024, 2000, 8192                                 41 / 32, 51 / 51, 91 / 159
+  //   of 2500 and 127, on 1024, 2000, 8192                               118 / 117, 157 / 167, 416 / 470
+  //   4 of 300 and 16, on 2000, 8192                                     69 / 62, 211 / 209
+  int64_t thin = 0;
   if (own_tall && G > 0 && prefix.max_len > 0) {
-    const double unfilled = std::max(0.0, (double)S - (double)pairs / kTall) * (double)heads;
-    const double steps = (double)((prefix.max_len + kTallStep - 1) / kTallStep);
+    const double steps = (double)((prefix.max_len + kTallStep - 1) / kTallStep), width = s.head_dim / 128.0;
+    const double unfilled = std::max(0.0, (double)S - (double)pairs / kTall);
+    const int64_t others = std::max<int64_t>(0, (pairs - kThin * S + longest - kThin - 1) / (longest - kThin));
+    const int64_t most = std::max<int64_t>(0, S - others);
+    thin = std::max<int64_t>(0, 2 * most - S);
+    const double work = std::max(unfilled * 0.0045, (double)thin * 0.0025) * (double)heads * steps * width;
+    const int tall = tall_chunk_of(std::max(S, pairs / kTall) * heads, tall_keys, pairs * heads, s.head_dim, false);
+    const double last = most == 0 ? 0.0 : steps * (0.14 + 0.46 * width) -
+                                              (double)(tall / kTallStep) * (0.6 + 0.003 * s.head_dim);
     const double parts = 5.0 + (double)(pairs * heads) * s.head_dim * 8.0 / 2.0e6;
-    p.alone = unfilled * steps * 0.0045 * s.head_dim / 128.0 < parts;
+    p.alone = work + std::max(0.0, last) < parts;
   }
   // A wave to a head, where there are heads enough to fill the device and the runs are short:
   // fewer workgroups to begin and end, less even work.  us, four waves / one to a head, runs of 5,
   // 64, 128, 192, 256 tokens, heads of 128: 576 runs and key heads 9.6 / 6.1, 9.9 / 7.6,
   // 11.6 / 10.2, 14.2 / 12.9, 15.9 / 15.5; 1120: 13.6 / 7.0, 15.0 / 10.2, 18.3 / 16.8, 22.7 / 24.1,
   // 26.4 / 30.8; 1920: 19.2 / 7.2, 22.5 / 11.8, 28.2 / 20.6, 35.3 / 29.4, 41.6 / 38.4.
-  p.spread = heads % kWaves == 0 && S * heads >= 512 && runs.max_len <= 192;
+  // (Where they take a prefix too, with its keys: 100 sequences of 1 to 10 rows, 32 heads on 8, on
+  // prefixes of 256 tokens 27 / 36.)
+  p.spread = heads % kWaves == 0 && S * heads >= 512 &&
+             (int64_t)runs.max_len + (p.alone && thin > 0 ? prefix.max_len : 0) <= 192;
   const int64_t units = p.spread ? heads / kWaves : heads;
   p.chunk_thin = thin_chunk_of((p.thin_tiled ? std::max(S, pairs / kThin) : S) * units, runs.max_len, prefix.max_len == 0);
   // Among prompts a thin tile that takes its whole run ends with their tiles, and nothing need be
@@ -1501,10 +1525,9 @@ AttendPlan plan_cache_attend(const CacheShape& s, const CacheRows& rows, const C
   p.thin_blocks = p.thin_tiles * units * (runs.max_len > 0 ? parts_of(runs.max_len, p.chunk_thin) : 1);
   p.short_parts = parts_of(runs.max_len, p.chunk_thin);
   if (own_tall) {
-    const int64_t keys = (prefix.max_len + kTallStep - 1) / kTallStep * kTallStep + (int64_t)runs.max_len;
     p.tall_tiles = (int)(pairs / kTall + S);
-    p.chunk_tall = tall_chunk_of(std::max(S, pairs / kTall) * heads, keys, pairs * heads, s.head_dim, false);
-    p.tall_parts = parts_of(keys, p.chunk_tall);
+    p.chunk_tall = tall_chunk_of(std::max(S, pairs / kTall) * heads, tall_keys, pairs * heads, s.head_dim, false);
+    p.tall_parts = parts_of(tall_keys, p.chunk_tall);
     p.tall_blocks = p.tall_tiles * heads * (p.tall_parts > 0 ? p.tall_parts : 1);
     if (p.tall_parts > p.short_parts) p.short_parts = p.tall_parts;
   }
