@@ -25,6 +25,13 @@
 //                     such a sequence fills tiles by itself, so sharing the prefix's
 //                     reads saves nothing and parts would only be written and read.
 // Where that is less work, all sequences of a batch take their prefixes so (ALONE).
+//
+// Scores, maxima, sums and outputs are float32.  A probability is rounded to the cache's type
+// where it meets its value: the bfloat16 matrix instructions take both operands so, and a second
+// product for the rest would be half as much work again in the tall tiles, which the matrix cores'
+// power bounds.  The thin tiles round alike, so that a row has one accuracy whatever batch it is
+// in.  The sum l takes the probabilities unrounded.  Against 64 bits the bfloat16 cases are off by
+// 2.1e-3 to 2.3e-3 of the output (root mean square), of which 1.65e-3 is the output's own rounding.
 #include <float.h>
 
 #include <algorithm>
@@ -496,7 +503,7 @@ struct KeyByKey {
         const float mn = fmaxf(m, sc), f = __builtin_amdgcn_exp2f(m - mn), w = __builtin_amdgcn_exp2f(sc - mn);
         m = mn;
         l = fmaf(l, f, w);
-        const float wt = (float)(T)w;
+        const float wt = (float)(T)w;                // (as in the tiles)
 #pragma unroll
         for (int g = 0; g < D / (4 * P); ++g) {
           const vec4 v = *reinterpret_cast<const vec4*>(V + sizeof(vec4) * (P * g + p));
@@ -680,7 +687,7 @@ __device__ __forceinline__ void thin_tile(const AttendArgs& a, char* smem, bool 
       if constexpr (sizeof(T) == 2) {
         bf16x4_t pb;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) pb[k] = (__bf16)p[k];
+        for (int k = 0; k < 4; ++k) pb[k] = (__bf16)p[k];            // (the one rounding of a weight)
 #pragma unroll
         for (int e = 0; e < D / 16; ++e) {
           const bf16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((ltr_t)(lds_t)(uintptr_t)(vsrc ^ e << 5));
@@ -887,7 +894,7 @@ __device__ __forceinline__ void weigh(Pairs<D>& w, const f32x16_t (&st)[2], bf16
   const float p1 = __builtin_amdgcn_exp2f(fmaf(st[e >> 3][2 * (e & 7) + 1], c2, -w.m));
   w.l += p0;
   w.l += p1;
-  bf16x2_t b = {(__bf16)p0, (__bf16)p1};
+  bf16x2_t b = {(__bf16)p0, (__bf16)p1};           // (the one rounding of a weight)
   pin(w.l, b);
   pb[e >> 2][2 * (e & 3)] = b[0];
   pb[e >> 2][2 * (e & 3) + 1] = b[1];
