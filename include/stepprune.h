@@ -508,7 +508,8 @@ typedef struct {
                                (SP_DEV_BAD_POSITION); its row is left out */
   int32_t rot_dim;          /* a multiple of 16, <= head_dim */
   int32_t interleaved;      /* 0 or 1 */
-  const int32_t* pos;       /* device [axes, rows], or NULL: the row's slot */
+  const int32_t* pos;       /* device [axes, rows], or NULL: the row's slot in its own run.  Slots begin
+                               at 0 behind a shared prefix too: its sequences pass their positions */
   int32_t axes;             /* 1 to 3 (pos NULL: 1) */
   int32_t section[3];       /* pairs of each axis, rot_dim / 2 in all */
 } sp_cache_rotation;
@@ -568,11 +569,12 @@ enum { SP_ATTEND_ALL = 1u };  /* every row sees its sequence's whole run */
  * order of the sums, so their rounding).  With prefixes and runs of length 0 this is cross
  * attention to the prefixes.
  *
- * A prefix is read once for the rows of all its sequences, except where reading it for each
- * is faster, by the bounds: for few sequences of up to 16 rows x (q_heads / kv_heads) on short
- * prefixes; for a sequence of more than 64 of them; and, where the longest sequence has more than
- * 16, for all sequences of the batch, unless their short ones would read long prefixes many
- * times or end behind the long ones.
+ * A prefix is read once for the rows of all its sequences, except where reading it for each is
+ * faster.  A sequence's rows times q_heads / kv_heads, its pairs, and the bounds decide: few
+ * sequences of up to 16 pairs on short prefixes read them each by itself, and so does every
+ * sequence of more than 64; where the longest has more than 16, all sequences of the batch do,
+ * unless the bounds leave room for so many short ones, or for prefixes so long, that these
+ * would take longer than the long sequences.
  *
  *  Q        [rows, q_heads head_dim], row stride ldq; 16-byte aligned
  *  rows, runs   the batch's sequences (runs->count = S)

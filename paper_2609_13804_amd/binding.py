@@ -329,7 +329,8 @@ def cache_runs(table, length, max_len) -> sp_cache_runs:
 
 def cache_rotation(cos_sin, rot_dim, pos=None, section=None, interleaved=False) -> sp_cache_rotation:
     """Rotation by position: float32 ``cos_sin`` [positions, rot_dim / 2, 2]; int32 ``pos``
-    [axes, rows] with the pairs of each axis in ``section``, or None: the rows' slots."""
+    [axes, rows] with the pairs of each axis in ``section``, or None: the rows' slots in their
+    own runs, which begin at 0 behind a shared prefix too."""
     section = [rot_dim // 2] if section is None else list(section)
     _read_as("cos_sin", cos_sin, "float32", 0)
     if hasattr(cos_sin, "numel") and cos_sin.numel() != cos_sin.shape[0] * rot_dim:

@@ -31,7 +31,7 @@
 // product for the rest would be half as much work again in the tall tiles, which the matrix cores'
 // power bounds.  The thin tiles round alike, so that a row has one accuracy whatever batch it is
 // in.  The sum l takes the probabilities unrounded.  Against 64 bits the bfloat16 cases are off by
-// 2.1e-3 to 2.3e-3 of the output (root mean square), of which 1.65e-3 is the output's own rounding.
+// 2.0e-3 to 2.3e-3 of the output (root mean square), of which 1.65e-3 is the output's own rounding.
 #include <float.h>
 
 #include <algorithm>
