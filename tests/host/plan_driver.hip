@@ -15,8 +15,8 @@ int main() {
                &runs.count, &runs.max_len, &prefix.count, &prefix.max_len) == 10) {
     rows.rows = n;
     const sp::AttendPlan p = sp::plan_cache_attend(s, rows, runs, prefix);
-    printf("alone %d wide %d spread %d prefix_parts %d tall_parts %d chunk_tall %d tall_tiles %d tall_blocks %lld\n",
-           p.alone, p.wide, p.spread, p.prefix_parts, p.tall_parts, p.chunk_tall, p.tall_tiles,
+    printf("alone %d wide %d spread %d prefix_parts %d short_parts %d chunk_thin %d tall_parts %d chunk_tall %d tall_tiles %d tall_blocks %lld\n",
+           p.alone, p.wide, p.spread, p.prefix_parts, p.short_parts, p.chunk_thin, p.tall_parts, p.chunk_tall, p.tall_tiles,
            (long long)p.tall_blocks);
   }
   return 0;
