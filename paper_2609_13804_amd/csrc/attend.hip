@@ -498,9 +498,12 @@ struct KeyByKey {
 #pragma unroll
         for (int j = 0; j < E; ++j) dot = fmaf((float)q[s][j], (float)k[j], dot);
       }
-      const float sc = (P == 2 ? half_sum(dot) : quad_sum(dot)) * a.c2;
+      const float st = P == 2 ? half_sum(dot) : quad_sum(dot);
       if (key < lim) {
-        const float mn = fmaxf(m, sc), f = __builtin_amdgcn_exp2f(m - mn), w = __builtin_amdgcn_exp2f(sc - mn);
+        const float mn = fmaxf(m, st * a.c2), f = __builtin_amdgcn_exp2f(m - mn);
+        float e = fmaf(st, a.c2, -mn);               // (as in the tiles)
+        if (sizeof(T) == 4 && st > kLowest) e = fmaf(st, a.c2_low, e);
+        const float w = __builtin_amdgcn_exp2f(e);
         m = mn;
         l = fmaf(l, f, w);
         const float wt = (float)(T)w;                // (as in the tiles)
@@ -509,8 +512,8 @@ struct KeyByKey {
           const vec4 v = *reinterpret_cast<const vec4*>(V + sizeof(vec4) * (P * g + p));
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const int e = 4 * g + k;
-            o[e / W][e % W] = fmaf(wt, (float)v[k], o[e / W][e % W] * f);
+            const int i = 4 * g + k;
+            o[i / W][i % W] = fmaf(wt, (float)v[k], o[i / W][i % W] * f);
           }
         }
       }
